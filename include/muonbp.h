@@ -430,6 +430,141 @@ const char* muonbp_adamw_last_error(const muonbp_adamw_ctx* ctx);
 void muonbp_adamw_destroy(muonbp_adamw_ctx* ctx); /* NULL is a no-op */
 
 /* ------------------------------------------------------------------------
+ * 8-bit linear layers: the products that read the weights and make the
+ * gradients the optimizer takes, with weights and activations held in 8-bit
+ * floating point, one power-of-two scale for each block of 128 values.
+ *
+ * For Y = X W (X: tokens x in, W: in x out, the layout of muonbp_matrix):
+ *   x8        = quantize(X)                 kept for the backward pass
+ *   w8, w8t   = quantize_weight(W)          after each optimizer step
+ *   Y         = product(x8, w8t)            tokens x out
+ *   dX        = product(quantize(dY), w8)   tokens x in
+ *   dW        = weight_grad(x8, dY)         in x out: muonbp_step's gradient
+ * and for a gated MLP, h = silu(gate) up with gate and up kept in 8 bits
+ * (gated_forward) and their gradients from what was kept (gated_backward).
+ *
+ * The value of element (r, c) of an 8-bit matrix is q 2^(s - 127): q the byte
+ * data[r * ld + c] read as e4m3 (MUONBP_E4M3, largest value 448, no infinity)
+ * or e5m2 (MUONBP_E5M2, largest value 57344), s byte (c / 128) % 4 (the lowest
+ * first) of the word scales[(c / 512) * scale_ld + r].  Quantizing takes, for
+ * each block of 128 columns of a row (of a weight: for each 128 x 128 tile),
+ * the smallest scale 2^e, e >= -110, with max |x| <= 2^e * largest value, and
+ * rounds x / 2^e to the nearest value, ties to even.  So no value overflows its
+ * type, scaling loses no bits, and every value is exact in bf16 and fp32 (but
+ * 2^128, to which an |x| over 1.9375 2^127 rounds: infinite there).  NaN and
+ * infinities do not count in the max: NaN stays NaN, an infinity becomes NaN in
+ * e4m3 and stays infinite in e5m2, and their block's other values keep their
+ * precision.  A block of zeros has e = -110.
+ *
+ * The conventions above apply (status codes, asynchrony on the context's
+ * stream, no synchronisation, thread safety).  A call allocates nothing, so it
+ * may be captured into a HIP graph.  Calls of one context share its workspace
+ * and run on its stream in order.  Outputs must not overlap inputs or each
+ * other (E_INVALID).  rows = 0 is valid everywhere (weight_grad over no tokens
+ * gives zeros); its pointers may then be NULL.
+ * ---------------------------------------------------------------------- */
+typedef enum { MUONBP_E4M3 = 0, MUONBP_E5M2 = 1 } muonbp_format;
+
+/* A device matrix in 16 or 32 bits: rows x cols, row r at ptr + r * ld elements
+ * (ld >= cols).  Any element-aligned pointer and any ld are accepted; rows that
+ * start at multiples of 16 bytes are faster in weight_grad. */
+typedef struct {
+  void* ptr;
+  int64_t rows, cols, ld;
+  muonbp_dtype dtype;
+} muonbp_dense;
+
+/* A device matrix in 8 bits as above.  data: rows x ld bytes, 16-byte aligned,
+ * ld a multiple of 16 and at least cols rounded up to 128; the bytes between
+ * cols and that are zeros (quantizing writes them, products read them).  scales:
+ * ceil(cols / 512) x scale_ld words, scale_ld >= rows; bytes past the last block
+ * are zeros.  Rows [a, b) of a matrix are the matrix {data + a * ld, scales + a,
+ * b - a, cols, ld, scale_ld, format}.  cols and ld at most 2^22. */
+typedef struct {
+  void* data;
+  uint32_t* scales;
+  int64_t rows, cols, ld, scale_ld;
+  int32_t format; /* muonbp_format */
+} muonbp_blocks;
+
+typedef struct {
+  int64_t workspace_bytes; /* device memory for the sums of products whose long
+                              axis is split over workgroups (default 64 MiB;
+                              0: never split)                                 */
+} muonbp_linear_options;
+
+typedef struct muonbp_linear_ctx muonbp_linear_ctx; /* opaque */
+
+/* Defaults.  NULL is ignored. */
+void muonbp_linear_options_default(muonbp_linear_options* opt);
+
+/* Create a context on the current device.  opt NULL for defaults.  Errors:
+ * E_INVALID (NULL out, negative workspace), E_NOMEM, E_HIP. */
+muonbp_status muonbp_linear_create(const muonbp_linear_options* opt, void* hip_stream,
+                                   muonbp_linear_ctx** out);
+
+/* out <- x in 8 bits.  x f32 or bf16; out of the same rows and cols.
+ * Errors of this and the calls below, before anything is enqueued: E_INVALID
+ * (NULL, misaligned or overlapping pointers, unknown format), E_SHAPE (sizes
+ * that do not match, cols < 1, ld or scale_ld too small or too large), E_DTYPE;
+ * E_STATE (poisoned context); E_HIP. */
+muonbp_status muonbp_linear_quantize(muonbp_linear_ctx* ctx, const muonbp_dense* x,
+                                     const muonbp_blocks* out);
+
+/* out <- w in 8 bits with one scale for each 128 x 128 tile, and out_t <- its
+ * transpose (the same values; cols x rows).  Either may be NULL, not both. */
+muonbp_status muonbp_linear_quantize_weight(muonbp_linear_ctx* ctx, const muonbp_dense* w,
+                                            const muonbp_blocks* out, const muonbp_blocks* out_t);
+
+/* out <- the values of x, exact in bf16 and f32. */
+muonbp_status muonbp_linear_restore(muonbp_linear_ctx* ctx, const muonbp_blocks* x,
+                                    const muonbp_dense* out);
+
+/* c <- a b^T (accumulate = 0) or c + a b^T (1): a is M x K in e4m3 or e5m2, b is
+ * N x K in e4m3, c M x N in bf16 or f32, rounded once from an fp32 sum.  For
+ * bf16 results the products of 64 values are added by the 8-bit matrix
+ * instructions, whose sum is 2^-16 of itself off (measured, 1.5e-5 in the
+ * 2-norm; 130 times finer than the result's rounding); for f32 results by the
+ * 16-bit ones, exact products in fp32 sums, at half the rate. */
+muonbp_status muonbp_linear_product(muonbp_linear_ctx* ctx, const muonbp_blocks* a,
+                                    const muonbp_blocks* b, const muonbp_dense* c,
+                                    int32_t accumulate);
+
+/* dw <- x^T dy (accumulate = 0) or dw + x^T dy (1): x is tokens x I in 8 bits
+ * (the kept activations), dy tokens x O in bf16, dw I x O in bf16 or f32.  The
+ * values of x are exact in bf16, so the only roundings are those of the fp32
+ * sum and of dw. */
+muonbp_status muonbp_linear_weight_grad(muonbp_linear_ctx* ctx, const muonbp_blocks* x,
+                                        const muonbp_dense* dy, const muonbp_dense* dw,
+                                        int32_t accumulate);
+
+/* h <- silu(gate) up, silu(g) = g / (1 + exp(-g)), all of one shape.  gate, up
+ * and h (NULL or dense) have one dtype, f32 or bf16; out8 (NULL or 8-bit)
+ * receives h in 8 bits; one of h and out8 is given.  gate_kept and up_kept (both
+ * or neither NULL) receive gate and up in 8 bits for gated_backward. */
+muonbp_status muonbp_linear_gated_forward(muonbp_linear_ctx* ctx, const muonbp_dense* gate,
+                                          const muonbp_dense* up, const muonbp_dense* h,
+                                          const muonbp_blocks* out8, const muonbp_blocks* gate_kept,
+                                          const muonbp_blocks* up_kept);
+
+/* The gradients of that at the kept gate g and up u, s = 1 / (1 + exp(-g)):
+ *   dgate = dh u s (1 + g (1 - s)),   dup = dh g s.
+ * dh, dgate and dup (both or neither NULL) have one dtype; dgate8 and dup8 (both
+ * or neither NULL) receive the gradients in 8 bits (from the unrounded values);
+ * one pair is given. */
+muonbp_status muonbp_linear_gated_backward(muonbp_linear_ctx* ctx, const muonbp_dense* dh,
+                                           const muonbp_blocks* gate, const muonbp_blocks* up,
+                                           const muonbp_dense* dgate, const muonbp_dense* dup,
+                                           const muonbp_blocks* dgate8, const muonbp_blocks* dup8);
+
+/* Change the stream used by later calls (waits for the old one: the workspace
+ * is shared). */
+muonbp_status muonbp_linear_set_stream(muonbp_linear_ctx* ctx, void* hip_stream);
+muonbp_status muonbp_linear_synchronize(muonbp_linear_ctx* ctx);
+const char* muonbp_linear_last_error(const muonbp_linear_ctx* ctx);
+void muonbp_linear_destroy(muonbp_linear_ctx* ctx); /* waits for its stream; NULL is a no-op */
+
+/* ------------------------------------------------------------------------
  * Learning-rate schedules of the paper's runs (Appendix B): cosine decay
  * (960M and 1.2B models) and warmup-stable-decay with a linear decay to a
  * final value (8B model; no warmup and a 20% cooldown for the 160M model).

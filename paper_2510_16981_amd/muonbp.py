@@ -15,6 +15,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libmuonbp.so")
 
 F32, BF16 = 0, 1
+E4M3, E5M2 = 0, 1
 KERNEL_KINDS = ("momentum", "scale", "pack", "gram", "poly", "apply", "update", "ns_span")
 NS_KINDS = ("gram", "poly", "apply")
 
@@ -66,6 +67,21 @@ class AdamwOptions(ctypes.Structure):
                 ("weight_decay", ctypes.c_float), ("max_grad_norm", ctypes.c_float),
                 ("param_dtype", ctypes.c_int), ("stream_hint", ctypes.c_int32),
                 ("algorithm", ctypes.c_int32)]
+
+
+class Dense(ctypes.Structure):
+    _fields_ = [("ptr", ctypes.c_void_p), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64),
+                ("ld", ctypes.c_int64), ("dtype", ctypes.c_int)]
+
+
+class BlocksRef(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("rows", ctypes.c_int64),
+                ("cols", ctypes.c_int64), ("ld", ctypes.c_int64), ("scale_ld", ctypes.c_int64),
+                ("format", ctypes.c_int32)]
+
+
+class LinearOptions(ctypes.Structure):
+    _fields_ = [("workspace_bytes", ctypes.c_int64)]
 
 
 class Profile(ctypes.Structure):
@@ -124,6 +140,19 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "muonbp_adamw_synchronize": (ctypes.c_int, [P]),
         "muonbp_adamw_last_error": (ctypes.c_char_p, [P]),
         "muonbp_adamw_destroy": (None, [P]),
+        "muonbp_linear_options_default": (None, [ctypes.POINTER(LinearOptions)]),
+        "muonbp_linear_create": (ctypes.c_int, [ctypes.POINTER(LinearOptions), P, ctypes.POINTER(P)]),
+        "muonbp_linear_quantize": (ctypes.c_int, [P, P, P]),
+        "muonbp_linear_quantize_weight": (ctypes.c_int, [P, P, P, P]),
+        "muonbp_linear_restore": (ctypes.c_int, [P, P, P]),
+        "muonbp_linear_product": (ctypes.c_int, [P, P, P, P, I32]),
+        "muonbp_linear_weight_grad": (ctypes.c_int, [P, P, P, P, I32]),
+        "muonbp_linear_gated_forward": (ctypes.c_int, [P] * 7),
+        "muonbp_linear_gated_backward": (ctypes.c_int, [P] * 8),
+        "muonbp_linear_set_stream": (ctypes.c_int, [P, P]),
+        "muonbp_linear_synchronize": (ctypes.c_int, [P]),
+        "muonbp_linear_last_error": (ctypes.c_char_p, [P]),
+        "muonbp_linear_destroy": (None, [P]),
         "muonbp_step_static": (ctypes.c_int, [ctypes.POINTER(Matrix), I32, ctypes.POINTER(P),
                                               ctypes.POINTER(P), P, I64, I64, F, F, F, F,
                                               ctypes.POINTER(Options), P]),
@@ -432,6 +461,207 @@ class AdamW:
     def close(self) -> None:
         if getattr(self, "ctx", None):
             self.lib.muonbp_adamw_destroy(self.ctx)
+            self.ctx = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+# ---------------------------------------------------------------- 8-bit linear layers
+
+BLOCK_COLS, GROUP_COLS = 128, 512
+
+
+class Blocks:
+    """A matrix in 8-bit floating point with a power-of-two scale for each
+    block of 128 columns of a row (muonbp_blocks): ``data`` is uint8, rows x
+    (cols rounded up to 128 at least), ``scales`` int32, ceil(cols / 512) x
+    rows, a byte for each block.  Holds its tensors; makes no copy."""
+
+    __slots__ = ("data", "scales", "rows", "cols", "format", "ref", "addr")
+
+    def __init__(self, data, scales, cols: int, format: int = E4M3):
+        import torch
+        rows = data.shape[0]
+        groups = -(-cols // GROUP_COLS)
+        if not (data.dim() == 2 and data.dtype == torch.uint8 and data.is_cuda and data.stride(1) == 1
+                and data.shape[1] >= -(-cols // BLOCK_COLS) * BLOCK_COLS):
+            raise ValueError(f"data: need a CUDA uint8 matrix with rows of at least {cols} bytes rounded up "
+                             f"to {BLOCK_COLS}, got {data.dtype} {tuple(data.shape)}")
+        if not (tuple(scales.shape) == (groups, rows) and scales.dtype == torch.int32
+                and scales.device == data.device and (rows <= 1 or scales.stride(1) == 1)):
+            raise ValueError(f"scales: need an int32 matrix of shape {(groups, rows)} on {data.device}, "
+                             f"got {scales.dtype} {tuple(scales.shape)}")
+        self.data, self.scales, self.rows, self.cols, self.format = data, scales, rows, int(cols), int(format)
+        self.ref = BlocksRef(data.data_ptr(), scales.data_ptr(), rows, cols,
+                             data.stride(0) if rows > 1 else data.shape[1],
+                             scales.stride(0) if groups > 1 else rows, format)
+        self.addr = ctypes.addressof(self.ref)
+
+    def __getitem__(self, rows: slice) -> "Blocks":
+        """Rows [a, b) as a matrix of the same memory."""
+        a, b, step = rows.indices(self.rows)
+        if step != 1:
+            raise ValueError("rows of Blocks have step 1")
+        return Blocks(self.data[a:max(a, b)], self.scales[:, a:max(a, b)], self.cols, self.format)
+
+
+class Linear:
+    """The 8-bit linear-layer operators on one stream (muonbp_linear_*).
+
+    Matrices are 2-D CUDA tensors with contiguous rows (any row stride of at
+    least cols), bf16 or fp32, or ``Blocks``.  Results not given by ``out`` are
+    allocated on the context's stream, on which every call is enqueued."""
+
+    def __init__(self, workspace_bytes: Optional[int] = None, stream=None):
+        import torch
+        self.lib = load_library()
+        if stream is None:
+            stream = torch.cuda.current_stream()
+        opts = LinearOptions()
+        self.lib.muonbp_linear_options_default(ctypes.byref(opts))
+        if workspace_bytes is not None:
+            opts.workspace_bytes = int(workspace_bytes)
+        ctx = ctypes.c_void_p()
+        st = self.lib.muonbp_linear_create(ctypes.byref(opts), ctypes.c_void_p(stream.cuda_stream),
+                                           ctypes.byref(ctx))
+        if st:
+            raise MuonBPError(st, "muonbp_linear_create")
+        self.ctx = ctx
+        self._stream = stream
+        self.device = stream.device
+        self._torch = torch
+        self._codes = {torch.float32: F32, torch.bfloat16: BF16}
+
+    # -- helpers
+    def _check(self, st: int, what: str):
+        if st:
+            detail = self.lib.muonbp_linear_last_error(self.ctx)
+            raise MuonBPError(st, f"{what}: {detail.decode() if detail else ''}")
+
+    def _dense(self, t, name: str) -> Dense:
+        code = self._codes.get(t.dtype)
+        if code is None or t.dim() != 2 or t.device != self.device:
+            raise ValueError(f"{name}: need a bf16 or fp32 matrix on {self.device}, got {t.dtype} "
+                             f"{tuple(t.shape)} on {t.device}")
+        rows, cols = t.shape
+        ld, inner = t.stride()
+        if (inner != 1 and cols > 1) or (ld < cols and rows > 1):
+            raise ValueError(f"{name}: need contiguous rows, got strides {t.stride()}")
+        return Dense(t.data_ptr(), rows, cols, ld if rows > 1 else cols, code)
+
+    def _blocks(self, b: Blocks, name: str):
+        if not isinstance(b, Blocks) or b.data.device != self.device:
+            raise ValueError(f"{name}: need Blocks on {self.device}")
+        return b.addr
+
+    def _empty(self, rows: int, cols: int, dtype):
+        torch = self._torch
+        if torch.cuda.current_stream(self.device) == self._stream:
+            return torch.empty((rows, cols), dtype=dtype, device=self.device)
+        with torch.cuda.stream(self._stream):
+            return torch.empty((rows, cols), dtype=dtype, device=self.device)
+
+    def empty_blocks(self, rows: int, cols: int, format: int = E4M3) -> Blocks:
+        """Uninitialised Blocks of rows x cols."""
+        torch = self._torch
+        return Blocks(self._empty(rows, -(-cols // BLOCK_COLS) * BLOCK_COLS, torch.uint8),
+                      self._empty(-(-cols // GROUP_COLS), rows, torch.int32), cols, format)
+
+    # -- API
+    def quantize(self, x, format: int = E4M3, out: Optional[Blocks] = None) -> Blocks:
+        """x in 8 bits, one scale for each block of 128 columns of a row."""
+        d = self._dense(x, "x")
+        if out is None:
+            out = self.empty_blocks(d.rows, d.cols, format)
+        self._check(self.lib.muonbp_linear_quantize(self.ctx, ctypes.addressof(d), self._blocks(out, "out")),
+                    "quantize")
+        return out
+
+    def quantize_weight(self, w, format: int = E4M3, out: Optional[Blocks] = None,
+                        out_t: Optional[Blocks] = None) -> Tuple[Blocks, Blocks]:
+        """(w, its transpose) in 8 bits, one scale for each 128 x 128 tile."""
+        d = self._dense(w, "w")
+        if out is None:
+            out = self.empty_blocks(d.rows, d.cols, format)
+        if out_t is None:
+            out_t = self.empty_blocks(d.cols, d.rows, format)
+        self._check(self.lib.muonbp_linear_quantize_weight(self.ctx, ctypes.addressof(d),
+                                                           self._blocks(out, "out"),
+                                                           self._blocks(out_t, "out_t")), "quantize_weight")
+        return out, out_t
+
+    def restore(self, x: Blocks, dtype=None, out=None):
+        """The values of x (bf16 by default), exact."""
+        a = self._blocks(x, "x")
+        if out is None:
+            out = self._empty(x.rows, x.cols, dtype or self._torch.bfloat16)
+        d = self._dense(out, "out")
+        self._check(self.lib.muonbp_linear_restore(self.ctx, a, ctypes.addressof(d)), "restore")
+        return out
+
+    def product(self, a: Blocks, b: Blocks, dtype=None, out=None, accumulate: bool = False):
+        """a b^T (bf16 by default); ``accumulate`` adds it to ``out``."""
+        pa, pb = self._blocks(a, "a"), self._blocks(b, "b")
+        if out is None:
+            if accumulate:
+                raise ValueError("accumulate needs out")
+            out = self._empty(a.rows, b.rows, dtype or self._torch.bfloat16)
+        d = self._dense(out, "out")
+        self._check(self.lib.muonbp_linear_product(self.ctx, pa, pb, ctypes.addressof(d), int(accumulate)),
+                    "product")
+        return out
+
+    def weight_grad(self, x: Blocks, dy, dtype=None, out=None, accumulate: bool = False):
+        """x^T dy (bf16 by default); ``accumulate`` adds it to ``out``."""
+        px, dd = self._blocks(x, "x"), self._dense(dy, "dy")
+        if out is None:
+            if accumulate:
+                raise ValueError("accumulate needs out")
+            out = self._empty(x.cols, dd.cols, dtype or self._torch.bfloat16)
+        d = self._dense(out, "out")
+        self._check(self.lib.muonbp_linear_weight_grad(self.ctx, px, ctypes.addressof(dd), ctypes.addressof(d),
+                                                       int(accumulate)), "weight_grad")
+        return out
+
+    def gated_forward(self, gate, up, blocks: bool = False, keep: bool = True, format: int = E4M3):
+        """(h, gate, up) with h = silu(gate) up of the inputs' dtype (``blocks``:
+        in 8 bits) and gate and up kept in 8 bits (None without ``keep``)."""
+        g, u = self._dense(gate, "gate"), self._dense(up, "up")
+        h = self.empty_blocks(g.rows, g.cols, format) if blocks else self._empty(g.rows, g.cols, gate.dtype)
+        dense = None if blocks else self._dense(h, "h")
+        g8, u8 = (self.empty_blocks(g.rows, g.cols, format) if keep else None for _ in range(2))
+        self._check(self.lib.muonbp_linear_gated_forward(
+            self.ctx, ctypes.addressof(g), ctypes.addressof(u), None if blocks else ctypes.addressof(dense),
+            h.addr if blocks else None, g8.addr if keep else None, u8.addr if keep else None), "gated_forward")
+        return h, g8, u8
+
+    def gated_backward(self, dh, gate: Blocks, up: Blocks, blocks: bool = False, format: int = E4M3):
+        """(dgate, dup) of dh's dtype, and with ``blocks`` both in 8 bits too."""
+        d = self._dense(dh, "dh")
+        pg, pu = self._blocks(gate, "gate"), self._blocks(up, "up")
+        dgate, dup = (self._empty(d.rows, d.cols, dh.dtype) for _ in range(2))
+        a, b = self._dense(dgate, "dgate"), self._dense(dup, "dup")
+        dgate8, dup8 = (self.empty_blocks(d.rows, d.cols, format) if blocks else None for _ in range(2))
+        self._check(self.lib.muonbp_linear_gated_backward(
+            self.ctx, ctypes.addressof(d), pg, pu, ctypes.addressof(a), ctypes.addressof(b),
+            dgate8.addr if blocks else None, dup8.addr if blocks else None), "gated_backward")
+        return (dgate, dup, dgate8, dup8) if blocks else (dgate, dup)
+
+    def set_stream(self, stream) -> None:
+        self._check(self.lib.muonbp_linear_set_stream(self.ctx, ctypes.c_void_p(stream.cuda_stream)),
+                    "set_stream")
+        self._stream = stream
+
+    def synchronize(self) -> None:
+        self._check(self.lib.muonbp_linear_synchronize(self.ctx), "synchronize")
+
+    def close(self) -> None:
+        if getattr(self, "ctx", None):
+            self.lib.muonbp_linear_destroy(self.ctx)
             self.ctx = None
 
     def __del__(self):
