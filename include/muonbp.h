@@ -467,7 +467,7 @@ typedef enum { MUONBP_E4M3 = 0, MUONBP_E5M2 = 1 } muonbp_format;
 
 /* A device matrix in 16 or 32 bits: rows x cols, row r at ptr + r * ld elements
  * (ld >= cols).  Any element-aligned pointer and any ld are accepted; rows that
- * start at multiples of 16 bytes are faster in weight_grad. */
+ * start at multiples of 16 bytes are faster. */
 typedef struct {
   void* ptr;
   int64_t rows, cols, ld;
@@ -531,7 +531,8 @@ muonbp_status muonbp_linear_product(muonbp_linear_ctx* ctx, const muonbp_blocks*
                                     int32_t accumulate);
 
 /* dw <- x^T dy (accumulate = 0) or dw + x^T dy (1): x is tokens x I in 8 bits
- * (the kept activations), dy tokens x O in bf16, dw I x O in bf16 or f32.  The
+ * (the kept activations), dy tokens x O in bf16 (ld at most 2^25), dw I x O in
+ * bf16 or f32.  The
  * values of x are exact in bf16, so the only roundings are those of the fp32
  * sum and of dw. */
 muonbp_status muonbp_linear_weight_grad(muonbp_linear_ctx* ctx, const muonbp_blocks* x,

@@ -299,6 +299,7 @@ muonbp_status muonbp_linear_weight_grad(muonbp_linear_ctx* c, const muonbp_block
   if (accumulate != 0 && accumulate != 1) return fail(c, MUONBP_E_INVALID, "accumulate must be 0 or 1");
   if (xr.rows != g.rows || o.rows != xr.cols || o.cols != g.cols)
     return fail(c, MUONBP_E_SHAPE, "dw = x^T dy: shapes do not match");
+  if (g.ld > (int64_t(1) << 25)) return fail(c, MUONBP_E_SHAPE, "dy: ld over 2^25");
   Spans sp;
   sp.blocks(xr, false);
   sp.dense(g, size_of(tg), false);

@@ -1,135 +1,866 @@
 // Matrix products of 8-bit linear layers: C = A B^T of two 8-bit matrices, and
 // the weight gradient dW = X^T dY of an 8-bit and a 16-bit one.
+#include <type_traits>
+#include <utility>
+
 #include "linear_device.h"
 
 namespace muonbp {
 
 namespace {
 
-constexpr int kThreads = 256;
+// ---------------------------------------------------------------- shared pieces
 
-__device__ __forceinline__ uint32_t scale_at(const BlocksRef& m, int64_t row, int64_t col) {
-  return gload<uint32_t, 4>(m.scales + col / kGroupCols * m.scale_ld + row) >> (8 * (col / kBlockCols % 4)) & 255u;
+typedef __attribute__((address_space(3))) void lds_void_t;
+
+constexpr int kBufferWord3 = 0x00020000;  // raw buffer, 32-bit data format
+
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const void* p, uint32_t bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, int(bytes), kBufferWord3);
 }
 
-template <typename T>
-__device__ __forceinline__ void finish(const DenseRef& c, int64_t row, int64_t col, float v, bool accumulate) {
-  T* p = static_cast<T*>(c.ptr) + row * c.ld + col;
-  if (accumulate) v += to_f(*p);
-  *p = T(v);
+// s_waitcnt immediate: at most n vector-memory operations of this wave are
+// outstanding.
+constexpr int vmcnt_imm(int n) { return (n & 15) | (7 << 4) | (15 << 8) | ((n >> 4) << 14); }
+
+// 16-byte LDS read issued without a compiler-inserted wait (which would wait
+// for every copy into LDS still in flight); lgkm_wait and hold complete it.
+template <int OFF>
+__device__ __forceinline__ u32x4_t lds_read16(uint32_t addr) {
+  u32x4_t v;
+  asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(v) : "v"(addr), "n"(OFF));
+  return v;
+}
+template <int OFF>
+__device__ __forceinline__ uint32_t lds_read4(uint32_t addr) {
+  uint32_t v;
+  asm volatile("ds_read_b32 %0, %1 offset:%2" : "=v"(v) : "v"(addr), "n"(OFF));
+  return v;
+}
+// f(integral_constant 0), ..., f(integral_constant N - 1).
+template <typename F, int... I>
+__device__ __forceinline__ void each_of(F&& f, std::integer_sequence<int, I...>) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, typename F>
+__device__ __forceinline__ void each(F&& f) {
+  each_of(f, std::make_integer_sequence<int, N>{});
+}
+__device__ __forceinline__ void lgkm_wait() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+// No use of v may move above this point.
+template <typename V>
+__device__ __forceinline__ void hold(V& v) {
+  asm volatile("" : "+v"(v));
 }
 
-// One 64 x 64 tile a workgroup, a 32 x 32 quarter a wave, operands straight from
-// memory: lane l has row l % 32 of A and of B and 32 of every 64 bytes.
-template <typename T, Fp8 F>
-__global__ __launch_bounds__(kThreads) void k_product(BlocksRef a, BlocksRef b, DenseRef c, bool accumulate) {
-  const int64_t wide = (c.cols + 63) / 64;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t m0 = blockIdx.x / wide * 64 + 32 * (wave >> 1), n0 = blockIdx.x % wide * 64 + 32 * (wave & 1);
-  const int64_t m = m0 + (lane & 31), n = n0 + (lane & 31);
-  f32x16_t acc = {};
-  for (int64_t k = 0; k < a.cols; k += 64) {
-    const int64_t at = k + 32 * (lane >> 5);
-    uint32_t x[8] = {}, y[8] = {};
-    uint32_t sx = 127, sy = 127;
-    if (m < a.rows) {
-      sx = scale_at(a, m, k);
+// Workgroup barrier without the fence of __syncthreads(), which would wait
+// for the copies that the pipeline keeps in flight.
+__device__ __forceinline__ void barrier_no_fence() { asm volatile("s_barrier" ::: "memory"); }
+
+__device__ __forceinline__ uint32_t lds_addr(const void* p) {
+  return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((const lds_void_t*)p));
+}
+
+// Which tile workgroup b of a grid of tall x wide tiles x parts runs.  Consecutive
+// workgroups go to the 8 XCDs in turn; each XCD gets a contiguous run of tiles,
+// taken `kGroupTall` tiles high, so that the tiles resident on one XCD share
+// rows and columns in its L2.
+struct TileAt {
+  int ti, tj, part;
+};
+constexpr int kXcds = 8, kGroupTall = 8;
+__device__ __forceinline__ TileAt tile_at(int b, int total, int tall, int wide, int parts) {
+  const int x = b % kXcds, q = total / kXcds, r = total % kXcds;
+  int pos = x * q + min(x, r) + b / kXcds;
+  TileAt t;
+  t.part = pos % parts;
+  pos /= parts;
+  const int per = kGroupTall * wide, g = pos / per, in = pos - g * per;
+  const int h = min(kGroupTall, tall - g * kGroupTall);
+  t.ti = g * kGroupTall + in % h;
+  t.tj = in / h;
+  return t;
+}
+
+// Stores a wave's C block (TM x TN blocks of 32 x 32 whose first MFMA operand
+// was the n side: lane l has row l % 32 and columns 8 q + 4 (l / 32) .. + 3 in
+// acc[i][j][4 q .. 4 q + 3]) through `st`, 32 x (32 TN + 4) floats of LDS of the
+// wave's own, so that rows are written in whole 8-element chunks.
+template <typename T, int TM, int TN>
+__device__ __forceinline__ void store_tile(f32x16_t (&acc)[TM][TN], float* st, const DenseRef& c, int64_t row0,
+                                           int64_t col0, bool accumulate) {
+  constexpr int P = 32 * TN + 4;
+  constexpr int CH = 4 * TN;  // 8-element chunks of a row
+  const int lane = threadIdx.x & 63;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = gload<uint32_t, 4>(a.data + m * a.ld + at + 4 * i);
-    }
-    if (n < b.rows) {
-      sy = scale_at(b, n, k);
+  for (int i = 0; i < TM; ++i) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) y[i] = gload<uint32_t, 4>(b.data + n * b.ld + at + 4 * i);
-    }
-    if constexpr (sizeof(T) == 2) {
-      i32x8_t xv, yv;
+    for (int j = 0; j < TN; ++j)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        xv[i] = int(x[i]);
-        yv[i] = int(y[i]);
+      for (int q = 0; q < 4; ++q)
+        *reinterpret_cast<f32x4_t*>(st + (lane & 31) * P + 32 * j + 8 * q + 4 * (lane >> 5)) =
+            f32x4_t{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+#pragma unroll
+    for (int p = 0; p < 32 * CH / 64; ++p) {
+      const int at = p * 64 + lane, r = at / CH, k = 8 * (at % CH);
+      const int64_t row = row0 + 32 * i + r, col = col0 + k;
+      const int64_t left = c.cols - col;
+      const int n = row < c.rows ? int(left < 0 ? 0 : left > 8 ? 8 : left) : 0;
+      if (n > 0) {
+        float f[8];
+        *reinterpret_cast<f32x4_t*>(f) = *reinterpret_cast<const f32x4_t*>(st + r * P + k);
+        *reinterpret_cast<f32x4_t*>(f + 4) = *reinterpret_cast<const f32x4_t*>(st + r * P + k + 4);
+        T* out = static_cast<T*>(c.ptr) + row * c.ld + col;
+        if (accumulate) {
+          float old[8];
+          load8(out, n, old);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) f[e] += old[e];
+        }
+        store8(out, n, f);
       }
-      acc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(xv, yv, acc, F == Fp8::E4M3 ? 0 : 1, 0, 0, int(sx), 0,
-                                                            int(sy));
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const u32x2_t x0 = widen4<F>(x[2 * i], scale_of(sx)), x1 = widen4<F>(x[2 * i + 1], scale_of(sx));
-        const u32x2_t y0 = widen4<Fp8::E4M3>(y[2 * i], scale_of(sy)), y1 = widen4<Fp8::E4M3>(y[2 * i + 1], scale_of(sy));
-        acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-            __builtin_bit_cast(bf16x8_t, u32x4_t{x0[0], x0[1], x1[0], x1[1]}),
-            __builtin_bit_cast(bf16x8_t, u32x4_t{y0[0], y0[1], y1[0], y1[1]}), acc, 0, 0, 0);
-      }
     }
-  }
-#pragma unroll
-  for (int v = 0; v < 16; ++v) {
-    const int64_t row = m0 + 8 * (v >> 2) + 4 * (lane >> 5) + (v & 3);
-    if (row < c.rows && n < c.cols) finish<T>(c, row, n, acc[v], accumulate);
   }
 }
 
-// One 64 x 64 tile of dW a workgroup; 16 tokens at a time go through LDS as
-// bf16, transposed.
-template <typename T, Fp8 F>
-__global__ __launch_bounds__(kThreads) void k_weight_grad(BlocksRef x, DenseRef dy, DenseRef dw, bool accumulate) {
-  __shared__ __attribute__((aligned(16))) uint16_t xs[64][16], ys[64][16];
-  const int64_t wide = (dw.cols + 63) / 64;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int64_t i0 = blockIdx.x / wide * 64, o0 = blockIdx.x % wide * 64;
-  const int wi = 32 * (wave >> 1), wo = 32 * (wave & 1);
-  f32x16_t acc = {};
-  for (int64_t t0 = 0; t0 < x.rows; t0 += 16) {
-    const int64_t t = t0 + (tid >> 4);
-    const int c = 4 * (tid & 15);
-    u32x2_t q = {0, 0};
-    if (t < x.rows && i0 + c < x.cols)
-      q = widen4<F>(gload<uint32_t, 4>(x.data + t * x.ld + i0 + c), scale_of(scale_at(x, t, i0 + c)));
-    xs[c][tid >> 4] = uint16_t(q[0]);
-    xs[c + 1][tid >> 4] = uint16_t(q[0] >> 16);
-    xs[c + 2][tid >> 4] = uint16_t(q[1]);
-    xs[c + 3][tid >> 4] = uint16_t(q[1] >> 16);
+// The parts of a tile whose long axis is split: every workgroup stores its
+// sums, the last to arrive adds them in the order of the parts (the result does
+// not depend on which is last) and goes on; the others end.  Sums are stored and
+// loaded 16 bytes a lane with the device-coherent policy of a relaxed atomic
+// (they bypass the per-XCD caches), and every store has completed before the
+// part is counted.  False: this workgroup is done.
+constexpr int kCoherent = 16;  // sc1
+constexpr int kMaxParts = 8;
+template <int TM, int TN, int W>
+__device__ __forceinline__ bool join_parts(f32x16_t (&acc)[TM][TN], const SplitSpace& split, int tile, int part,
+                                           int parts, int wave, int lane, int* last) {
+  constexpr int WAVE = TM * TN * 16 * 64;  // sums of a wave
+  float* const all = split.sums + size_t(tile) * parts * (WAVE * W) + wave * WAVE;
+  auto span = [&](int p) { return buffer(all + size_t(p) * (WAVE * W), 4 * WAVE); };
+  const __amdgpu_buffer_rsrc_t mine = span(part);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int64_t o = o0 + c + e;
-      ys[c + e][tid >> 4] = t < x.rows && o < dy.cols
-                                ? gload<uint16_t, 2>(static_cast<const uint16_t*>(dy.ptr) + t * dy.ld + o)
-                                : uint16_t(0);
+  for (int q = 0; q < TM * TN; ++q)
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+      const f32x16_t& a = acc[q / TN][q % TN];
+      __builtin_amdgcn_raw_buffer_store_b128(
+          u32x4_t{f_bits(a[4 * v]), f_bits(a[4 * v + 1]), f_bits(a[4 * v + 2]), f_bits(a[4 * v + 3])}, mine,
+          ((q * 4 + v) * 64 + lane) * 16, 0, kCoherent);
     }
-    __syncthreads();
-    const bf16x8_t p = *reinterpret_cast<const bf16x8_t*>(&xs[wi + (lane & 31)][8 * (lane >> 5)]);
-    const bf16x8_t r = *reinterpret_cast<const bf16x8_t*>(&ys[wo + (lane & 31)][8 * (lane >> 5)]);
-    acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(p, r, acc, 0, 0, 0);
-    __syncthreads();
+  __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+  __syncthreads();
+  if (threadIdx.x == 0)
+    *last = __hip_atomic_fetch_add(split.counts + tile, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == parts - 1;
+  __syncthreads();
+  if (!*last) return false;
+  for (int p = 0; p < parts; ++p) {
+    const __amdgpu_buffer_rsrc_t from = span(p);
+#pragma unroll
+    for (int q = 0; q < TM * TN; ++q)
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        f32x16_t& a = acc[q / TN][q % TN];
+        const u32x4_t x = __builtin_amdgcn_raw_buffer_load_b128(from, ((q * 4 + v) * 64 + lane) * 16, 0, kCoherent);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) a[4 * v + e] = p == 0 ? bits_f(x[e]) : a[4 * v + e] + bits_f(x[e]);
+      }
+  }
+  if (threadIdx.x == 0) __hip_atomic_store(split.counts + tile, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return true;
+}
+
+// ---------------------------------------------------------------- product, ring of K slices
+//
+// A tile of BM x BN, K in slices of 64 bytes copied straight into a ring of 4
+// slots in LDS (rows of 64 bytes; 16-byte chunk c of row r at c ^ swz(r), which
+// spreads the 32 rows one fragment read touches over all banks).  WM x WN waves
+// hold blocks of 32 TM x 32 TN.  While the MFMAs of slice kt run, its
+// successor is read into the other set of fragment registers and the slot
+// that kt came from is refilled with slice kt + 4: one barrier a slice, right
+// after its first MFMA.
+//
+// The matrix instruction multiplies 32 x 64 by 64 x 32 in 8 bits and applies a
+// power-of-two scale per row and 32 columns: with the block scales fed to it,
+// the scaled product costs what an unscaled one does.  The words of scales of a
+// tile's rows (4 blocks: 8 slices) are copied into LDS a group ahead, and read
+// into registers when their group begins.
+//
+// EXACT (fp32 results): the fragments are widened to bf16, scales included,
+// which is exact, and multiplied by 16-bit instructions at half the rate,
+// because the 8-bit instruction's sum of 64 products keeps 16 bits (measured:
+// 1.5e-5 off at K from 64 to 16384, against 5e-8 of an fp32 product).
+__device__ __forceinline__ int swz(int row) { return ((row >> 1) & 3) ^ ((row >> 3) & 1); }
+
+template <typename T, Fp8 F, int TM, int TN, int WM, int WN>
+__global__ __launch_bounds__(64 * WM * WN) void k_product(BlocksRef a, BlocksRef b, DenseRef c, bool accumulate,
+                                                          int parts, SplitSpace split) {
+  constexpr bool EXACT = sizeof(T) == 4;
+  constexpr int BM = 32 * TM * WM, BN = 32 * TN * WN, W = WM * WN, NS = 4, ROW = 64;
+  constexpr int STAGE = (BM + BN) * ROW;
+  constexpr int LP = (BM + BN) / 16 / W;  // 1 KB copies (16 rows) of a slice per wave
+  constexpr int RS = (BM + BN) / 64;      // copies of 64 scale words
+  constexpr int LS = (RS + W - 1) / W;
+  static_assert(BM % (16 * W) == 0 && BN % (16 * W) == 0, "a wave's copy is all A or all B");
+  constexpr int EPI = W * 32 * (32 * TN + 4) * 4;
+  constexpr int RING = NS * STAGE > EPI ? NS * STAGE : EPI;
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[RING + 2 * (BM + BN) * 4];
+  __shared__ int last;
+  uint32_t* const words = reinterpret_cast<uint32_t*>(lds + RING);
+
+  const int tall = int((c.rows + BM - 1) / BM), wide = int((c.cols + BN - 1) / BN);
+  const TileAt t = tile_at(blockIdx.x, gridDim.x, tall, wide, parts);
+  const int64_t m0 = int64_t(t.ti) * BM, n0 = int64_t(t.tj) * BN;
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave / WN, wn = wave % WN;
+  const int ma = int(min(int64_t(BM), a.rows - m0)), nb = int(min(int64_t(BN), b.rows - n0));
+  const uint32_t kbytes = uint32_t((a.cols + kBlockCols - 1) / kBlockCols * kBlockCols);
+  const uint32_t abytes = uint32_t(ma - 1) * uint32_t(a.ld) + kbytes;
+  const uint32_t bbytes = uint32_t(nb - 1) * uint32_t(b.ld) + kbytes;
+  const __amdgpu_buffer_rsrc_t ar = buffer(a.data + m0 * a.ld, abytes), br = buffer(b.data + n0 * b.ld, bbytes);
+
+  // Slices of this part: whole blocks of 128.
+  const int nblk = int(kbytes / kBlockCols);
+  const int kb = 2 * int(int64_t(t.part) * nblk / parts), ke = 2 * int(int64_t(t.part + 1) * nblk / parts);
+
+  uint32_t voff[LP];
+#pragma unroll
+  for (int j = 0; j < LP; ++j) {
+    const int row = 16 * (wave + W * j) + (lane >> 2), col = 16 * ((lane & 3) ^ swz(row));
+    if (W * j < BM / 16)
+      voff[j] = row < ma ? uint32_t(row) * uint32_t(a.ld) + col : abytes;  // past the end: zeros
+    else
+      voff[j] = row - BM < nb ? uint32_t(row - BM) * uint32_t(b.ld) + col : bbytes;
+  }
+  // Copy j of slice kt into its slot.  Past the part's end the last slice is
+  // copied again (never read), so that every wait is a constant count.
+  auto copy = [&](int kt, int j) {
+    lds_void_t* dst = (lds_void_t*)(lds + (kt & (NS - 1)) * STAGE + (wave + W * j) * 1024);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(W * j < BM / 16 ? ar : br, dst, 16, int(voff[j]),
+                                             min(kt, ke - 1) * ROW, 0, 0);
+  };
+  const int groups = int((a.cols + kGroupCols - 1) / kGroupCols);
+  auto copy_scales = [&](int g) {
+#pragma unroll
+    for (int j = 0; j < LS; ++j) {
+      const int u = (wave + W * j) % RS;
+      const bool of_a = u < BM / 64;
+      const BlocksRef& m = of_a ? a : b;
+      const int64_t r0 = of_a ? m0 : n0;
+      const __amdgpu_buffer_rsrc_t r =
+          buffer(m.scales + int64_t(min(g, groups - 1)) * m.scale_ld + r0, 4u * uint32_t(of_a ? ma : nb));
+      lds_void_t* dst = (lds_void_t*)(words + (g & 1) * (BM + BN) + 64 * u);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, dst, 4, 4 * (64 * (of_a ? u : u - BM / 64) + lane), 0, 0, 0);
+    }
+  };
+
+  f32x16_t acc[TM][TN];
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int j = 0; j < TN; ++j) acc[i][j] = f32x16_t{};
+
+  constexpr int NF = TM + TN, NM = TM * TN, NR = 2 * NF;
+  // A fragment is 32 rows, which leaves the swizzle as it is: lane addresses
+  // of the first fragment of A and of B, half h, and constant offsets.
+  uint32_t fa[2][2], wa[2];
+#pragma unroll
+  for (int side = 0; side < 2; ++side) {
+    const int r = (side ? BM + wn * 32 * TN : wm * 32 * TM) + (lane & 31);
+    wa[side] = lds_addr(words) + 4 * r;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) fa[side][h] = lds_addr(lds) + r * ROW + (((2 * h + (lane >> 5)) ^ swz(r)) << 4);
+  }
+  u32x4_t fr[2][NF][2];
+  uint32_t sw[NF];
+  auto read_words = [&](int g) {
+    const uint32_t base = (g & 1) * (4 * (BM + BN));
+    each<NF>([&](auto o) {
+      constexpr int f = o;
+      sw[f] = lds_read4<128 * (f < TM ? f : f - TM)>(wa[f < TM ? 0 : 1] + base);
+    });
+  };
+  auto read_frag = [&](auto o, u32x4_t (&to)[NF][2], uint32_t base) {
+    constexpr int f = o / 2, h = o % 2, side = f < TM ? 0 : 1;
+    to[f][h] = lds_read16<32 * ROW * (f < TM ? f : f - TM)>(fa[side][h] + base);
+  };
+
+#pragma unroll
+  for (int s = 0; s < 2; ++s) copy_scales((kb >> 3) + s);
+#pragma unroll
+  for (int s = 0; s < NS; ++s)
+#pragma unroll
+    for (int j = 0; j < LP; ++j) copy(kb + s, j);
+  __builtin_amdgcn_s_waitcnt(vmcnt_imm((NS - 1) * LP));
+  barrier_no_fence();
+  each<NR>([&](auto o) { read_frag(o, fr[0], (kb & (NS - 1)) * STAGE); });
+  read_words(kb >> 3);
+  lgkm_wait();
+#pragma unroll
+  for (int f = 0; f < NF; ++f) {
+    hold(fr[0][f][0]);
+    hold(fr[0][f][1]);
+    hold(sw[f]);
+  }
+
+  auto slice = [&](auto set, int kt) {
+    constexpr int P = decltype(set)::value;
+    const int shift = 8 * (kt >> 1 & 3);
+    uint32_t sb[NF];
+#pragma unroll
+    for (int f = 0; f < NF; ++f) sb[f] = sw[f] >> shift;
+    u32x4_t wide_[EXACT ? NF : 1][4];
+    if constexpr (EXACT) {
+#pragma unroll
+      for (int f = 0; f < NF; ++f) {
+        const float s = scale_of(sb[f] & 255u);
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            u32x2_t x, y;
+            if (f < TM) {
+              x = widen4<F>(fr[P][f][h][2 * e], s);
+              y = widen4<F>(fr[P][f][h][2 * e + 1], s);
+            } else {
+              x = widen4<Fp8::E4M3>(fr[P][f][h][2 * e], s);
+              y = widen4<Fp8::E4M3>(fr[P][f][h][2 * e + 1], s);
+            }
+            wide_[f][2 * h + e] = u32x4_t{x[0], x[1], y[0], y[1]};
+          }
+      }
+    }
+    auto mfma = [&](int q) {
+      const int i = q / TN, j = q % TN;
+      if constexpr (EXACT) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, wide_[TM + j][e]),
+                                                              __builtin_bit_cast(bf16x8_t, wide_[i][e]), acc[i][j], 0,
+                                                              0, 0);
+      } else {
+        const u32x4_t *y = fr[P][TM + j], *x = fr[P][i];
+        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
+            i32x8_t{int(y[0][0]), int(y[0][1]), int(y[0][2]), int(y[0][3]), int(y[1][0]), int(y[1][1]), int(y[1][2]),
+                    int(y[1][3])},
+            i32x8_t{int(x[0][0]), int(x[0][1]), int(x[0][2]), int(x[0][3]), int(x[1][0]), int(x[1][1]), int(x[1][2]),
+                    int(x[1][3])},
+            acc[i][j], 0, F == Fp8::E4M3 ? 0 : 1, 0, int(sb[TM + j]), 0, int(sb[i]));
+      }
+    };
+    mfma(0);
+    __builtin_amdgcn_sched_barrier(0);
+    // Slice kt + 1 has landed for this wave, after the barrier for every wave;
+    // and every wave holds slice kt in registers, so its slot takes kt + 4.
+    __builtin_amdgcn_s_waitcnt(vmcnt_imm((NS - 2) * LP));
+    barrier_no_fence();
+    constexpr int R = NM - 1, RR = R > 2 ? R - 1 : R;  // the last MFMA hides the last reads
+    const uint32_t base = ((kt + 1) & (NS - 1)) * STAGE;
+    each<R>([&](auto at) {
+      mfma(at + 1);
+      each<NR>([&](auto o) {
+        if constexpr (o >= at * NR / RR && o < (at + 1) * NR / RR) read_frag(o, fr[P ^ 1], base);
+      });
+      each<LP>([&](auto o) {
+        if constexpr (o >= at * LP / R && o < (at + 1) * LP / R) copy(kt + NS, o);
+      });
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    lgkm_wait();
+#pragma unroll
+    for (int f = 0; f < NF; ++f) {
+      hold(fr[P ^ 1][f][0]);
+      hold(fr[P ^ 1][f][1]);
+    }
+  };
+  // A group of 8 slices shares its words of scales.  The inner loop has no
+  // other branch, so that its MFMAs stay between its reads and copies.
+  for (int kt = kb; kt < ke;) {
+    const int g = kt >> 3, end = min(8 * g + 8, ke);
+    for (; kt < end; kt += 2) {  // an even count: whole blocks
+      slice(std::integral_constant<int, 0>{}, kt);
+      slice(std::integral_constant<int, 1>{}, kt + 1);
+    }
+    // The words of group g + 1 were copied a whole group ago (or before the
+    // first slice); every wave has read those of group g, so their place takes
+    // the words of group g + 2.
+    copy_scales(g + 2);
+    read_words(g + 1);
+    lgkm_wait();
+#pragma unroll
+    for (int f = 0; f < NF; ++f) hold(sw[f]);
+  }
+  __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));  // copies past the end land before the ring is reused
+  if (parts > 1 && !join_parts<TM, TN, W>(acc, split, t.ti * wide + t.tj, t.part, parts, wave, lane, &last)) return;
+  __syncthreads();
+  store_tile<T, TM, TN>(acc, reinterpret_cast<float*>(lds) + wave * 32 * (32 * TN + 4), c,
+                        m0 + wm * 32 * TM, n0 + wn * 32 * TN, accumulate);
+}
+
+// ---------------------------------------------------------------- product, few rows
+//
+// C = A B^T for up to 16 rows of A (single tokens): bound by reading B once.
+// One workgroup holds 16 rows of B; its waves take the groups of 512 columns in
+// turn, straight from memory into registers (16 bytes a lane, 64 contiguous
+// bytes of a row an instruction) with the next group on its way, and their sums
+// meet in LDS.  Measured, one row: 14336 x 4096 14.5 us (4.0 TB/s), 4096 x 14336
+// 11.2 us (5.2 TB/s); 2 and 8 waves took 14.7 and 16.8, 12.5 and 11.1 us, and
+// columns split over 2 or 4 workgroups 13.9 and 23 us, 13.1 and 14.1 us.
+constexpr int kFewRows = 16, kFewWaves = 4;
+
+template <typename T, Fp8 F>
+__global__ __launch_bounds__(64 * kFewWaves) void k_product_few(BlocksRef a, BlocksRef b, DenseRef c,
+                                                                bool accumulate) {
+  constexpr bool EXACT = sizeof(T) == 4;
+  __shared__ __attribute__((aligned(16))) f32x4_t sums[kFewWaves][64];
+  const int lane = threadIdx.x & 63, waves = blockDim.x >> 6;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t n0 = int64_t(blockIdx.x) * 16;
+  const int nr = int(min(int64_t(16), b.rows - n0)), mr = int(a.rows);
+  const uint32_t kbytes = uint32_t((a.cols + kBlockCols - 1) / kBlockCols * kBlockCols);
+  const int blocks = int(kbytes / kBlockCols), groups = (blocks + 3) / 4;
+  const uint32_t bbytes = uint32_t(nr - 1) * uint32_t(b.ld) + kbytes;
+  const uint32_t abytes = uint32_t(mr - 1) * uint32_t(a.ld) + kbytes;
+  const __amdgpu_buffer_rsrc_t br = buffer(b.data + n0 * b.ld, bbytes), ar = buffer(a.data, abytes);
+  const int row = lane & 15, col = 16 * (lane >> 4);
+  const uint32_t boff = row < nr ? uint32_t(row) * uint32_t(b.ld) + col : bbytes;  // past the end: zeros
+  const uint32_t aoff = row < mr ? uint32_t(row) * uint32_t(a.ld) + col : abytes;
+
+  struct Group {
+    u32x4_t y[4][2], x[4][2];
+    uint32_t sy, sx;
+  };
+  auto load = [&](Group& r, int g) {
+    const __amdgpu_buffer_rsrc_t sb = buffer(b.scales + int64_t(g) * b.scale_ld + n0, 4u * uint32_t(nr));
+    const __amdgpu_buffer_rsrc_t sa = buffer(a.scales + int64_t(g) * a.scale_ld, 4u * uint32_t(mr));
+    r.sy = __builtin_amdgcn_raw_buffer_load_b32(sb, 4 * row, 0, 0);
+    r.sx = __builtin_amdgcn_raw_buffer_load_b32(sa, 4 * row, 0, 0);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int at = min(4 * g + k, blocks - 1) * kBlockCols;  // past the last block: it again, not used
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        r.y[k][h] = __builtin_amdgcn_raw_buffer_load_b128(br, int(boff), at + 64 * h, 0);
+        r.x[k][h] = __builtin_amdgcn_raw_buffer_load_b128(ar, int(aoff), at + 64 * h, 0);
+      }
+    }
+  };
+  f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
+  auto multiply = [&](const Group& r, int g) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if (4 * g + k >= blocks) break;
+      const uint32_t sy = r.sy >> (8 * k) & 255u, sx = r.sx >> (8 * k) & 255u;
+      const u32x4_t *y = r.y[k], *x = r.x[k];
+      if constexpr (EXACT) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const u32x2_t p = widen4<Fp8::E4M3>(y[h][2 * e], scale_of(sy)),
+                          q = widen4<Fp8::E4M3>(y[h][2 * e + 1], scale_of(sy));
+            const u32x2_t u = widen4<F>(x[h][2 * e], scale_of(sx)), w = widen4<F>(x[h][2 * e + 1], scale_of(sx));
+            acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                __builtin_bit_cast(bf16x8_t, u32x4_t{p[0], p[1], q[0], q[1]}),
+                __builtin_bit_cast(bf16x8_t, u32x4_t{u[0], u[1], w[0], w[1]}), acc, 0, 0, 0);
+          }
+      } else {
+        acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
+            i32x8_t{int(y[0][0]), int(y[0][1]), int(y[0][2]), int(y[0][3]), int(y[1][0]), int(y[1][1]), int(y[1][2]),
+                    int(y[1][3])},
+            i32x8_t{int(x[0][0]), int(x[0][1]), int(x[0][2]), int(x[0][3]), int(x[1][0]), int(x[1][1]), int(x[1][2]),
+                    int(x[1][3])},
+            acc, 0, F == Fp8::E4M3 ? 0 : 1, 0, int(sy), 0, int(sx));
+      }
+    }
+  };
+  int g = wave;
+  if (g < groups) {
+    Group r[2];
+    load(r[0], g);
+    for (; g < groups; g += 2 * waves) {
+      if (g + waves < groups) load(r[1], g + waves);
+      multiply(r[0], g);
+      if (g + waves >= groups) break;
+      if (g + 2 * waves < groups) load(r[0], g + 2 * waves);
+      multiply(r[1], g + waves);
+    }
+  }
+  sums[wave][lane] = acc;
+  __syncthreads();
+  if (wave > 0) return;
+  f32x4_t v = sums[0][lane];
+  for (int w = 1; w < waves; ++w) v += sums[w][lane];
+  const int64_t n = n0 + 4 * (lane >> 4);
+  if (row >= mr) return;
+  T* out = static_cast<T*>(c.ptr) + row * c.ld + n;
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (n + e < c.cols) {
+      float f = v[e];
+      if (accumulate) f += to_f(out[e]);
+      out[e] = T(f);
+    }
+}
+
+// ---------------------------------------------------------------- weight gradient
+//
+// dW = X^T dY over slices of 32 tokens.  A slice of X (8 bits) and of dY (16
+// bits) is loaded into registers two slices ahead, X is widened to bf16 with
+// its block's scale (exact; a thread's 16 values are one token's, so they share
+// it, which they would not along the tokens), and both are written to one of two
+// slots in LDS as they lie in memory: 32 rows (tokens) of BM or BN elements,
+// 16-byte chunk c of row r at c ^ 4 (r % 4).  The operands of the 16-bit matrix
+// instruction, 8 consecutive tokens of one feature a lane, come from LDS
+// transpose reads.  One barrier a slice.
+//
+// Loads are of any alignment.  Only the last tokens, where a row's last 16 bytes
+// may end past the matrix, are read an element at a time; a part begins with its
+// last two slices, so that the loop's loads are the same for every slice (with a
+// choice between them the compiler waits for all loads in flight at each).
+__device__ __forceinline__ int row_swz(int r) { return 4 * (r & 3); }
+
+// Each group of 16 lanes reads a 4 x 16 block of 16-bit elements; lane i gives
+// the address of elements 4 (i % 4) .. + 3 of row i / 4 and receives column i.
+template <int OFF>
+__device__ __forceinline__ u32x2_t lds_read8_tr(uint32_t addr) {
+  u32x2_t v;
+  asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(v) : "v"(addr), "n"(OFF));
+  return v;
+}
+
+template <typename T, Fp8 F, int TM, int TN, int WM, int WN>
+__global__ __launch_bounds__(64 * WM * WN) void k_weight_grad(BlocksRef x, DenseRef dy, DenseRef dw, bool accumulate,
+                                                              int parts, SplitSpace split) {
+  constexpr int BM = 32 * TM * WM, BN = 32 * TN * WN, W = WM * WN, NT = 64 * W, KT = 32;
+  constexpr int XP = 2 * BM, YP = 2 * BN, STAGE = KT * (XP + YP);  // bytes
+  constexpr int XC = KT * BM / 16 / NT, YC = KT * BN / 8 / NT;     // 16-byte loads per thread and slice
+  static_assert(XC * 16 * NT == KT * BM && YC * 8 * NT == KT * BN && BM % 128 == 0 && BN % 128 == 0, "tile");
+  constexpr int EPI = W * 32 * (32 * TN + 4) * 4;
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[2 * STAGE > EPI ? 2 * STAGE : EPI];
+  __shared__ int last;
+
+  const int tall = int((dw.rows + BM - 1) / BM), wide = int((dw.cols + BN - 1) / BN);
+  const TileAt t = tile_at(blockIdx.x, gridDim.x, tall, wide, parts);
+  const int64_t i0 = int64_t(t.ti) * BM, o0 = int64_t(t.tj) * BN;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave / WN, wn = wave % WN;
+  // Slices of this part, in the order ke - 1, ke - 2, kb, kb + 1, ...
+  const int64_t tokens = x.rows;
+  const int64_t nk = (tokens + KT - 1) / KT;
+  const int64_t kb = t.part * nk / parts, ke = (t.part + 1) * nk / parts;
+  const int count = int(ke - kb);
+
+  const int64_t padded = (x.cols + kBlockCols - 1) / kBlockCols * kBlockCols;
+  uint32_t xoff[XC], xlds[XC], yoff[YC], ylds[YC];
+  int xt[XC], yt[YC], ycol[YC];
+  uint32_t xshift[XC];
+#pragma unroll
+  for (int j = 0; j < XC; ++j) {
+    const int u = tid + NT * j, c = u % (BM / 16);
+    xt[j] = u / (BM / 16);
+    // Features past the padded columns: those of the first chunk instead
+    // (rows of dW that are not stored).
+    xoff[j] = uint32_t(xt[j]) * uint32_t(x.ld) + (i0 + 16 * c < padded ? 16 * c : 0);
+    xshift[j] = 8 * uint32_t((i0 / kBlockCols + c / 8) % 4);
+    xlds[j] = lds_addr(lds) + xt[j] * XP + (((2 * c) ^ row_swz(xt[j])) << 4);
   }
 #pragma unroll
-  for (int v = 0; v < 16; ++v) {
-    const int64_t row = i0 + wi + 8 * (v >> 2) + 4 * (lane >> 5) + (v & 3), col = o0 + wo + (lane & 31);
-    if (row < dw.rows && col < dw.cols) finish<T>(dw, row, col, acc[v], accumulate);
+  for (int j = 0; j < YC; ++j) {
+    const int u = tid + NT * j, c = u % (BN / 8);
+    yt[j] = u / (BN / 8);
+    ycol[j] = o0 + 8 * c < dy.cols ? 8 * c : 0;
+    yoff[j] = 2 * (uint32_t(yt[j]) * uint32_t(dy.ld) + uint32_t(ycol[j]));
+    ylds[j] = lds_addr(lds) + KT * XP + yt[j] * YP + ((c ^ row_swz(yt[j])) << 4);
   }
+  const uint8_t* const xbase = x.data + i0;
+  const uint32_t* const sbase = x.scales + i0 / kGroupCols * x.scale_ld;
+  const uint16_t* const ybase = static_cast<const uint16_t*>(dy.ptr) + o0;
+
+  struct Set {
+    u32x4_t x[XC], y[YC];
+    uint32_t s[XC];
+  };
+  Set in[2];
+  // Slice k: at least 8 tokens follow it, so a 16-byte load that passes the end
+  // of its row stays inside the matrix.
+  auto load_inner = [&](Set& r, int64_t k) {
+    const int64_t t0 = k * KT;
+#pragma unroll
+    for (int j = 0; j < XC; ++j) {
+      r.x[j] = gload<u32x4_t, 16>(xbase + t0 * x.ld + xoff[j]);
+      r.s[j] = gload<uint32_t, 4>(sbase + t0 + xt[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < YC; ++j)
+      r.y[j] = gload<u32x4_t, 2>(reinterpret_cast<const unsigned char*>(ybase + t0 * dy.ld) + yoff[j]);
+  };
+  auto load_any = [&](Set& r, int64_t k) {
+    const int64_t t0 = k * KT;
+    if (t0 + KT + 8 <= tokens) return load_inner(r, k);
+#pragma unroll
+    for (int j = 0; j < XC; ++j) {
+      r.x[j] = u32x4_t{0, 0, 0, 0};
+      r.s[j] = 0;
+      if (t0 + xt[j] < tokens) {
+        r.x[j] = gload<u32x4_t, 16>(xbase + t0 * x.ld + xoff[j]);
+        r.s[j] = gload<uint32_t, 4>(sbase + t0 + xt[j]);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < YC; ++j) {
+      r.y[j] = u32x4_t{0, 0, 0, 0};
+      if (t0 + yt[j] < tokens) {
+        const uint16_t* p = ybase + (t0 + yt[j]) * dy.ld + ycol[j];
+        const int64_t n = dy.cols - o0 - ycol[j];
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (e < n) r.y[j][e / 2] |= uint32_t(gload<uint16_t, 2>(p + e)) << (16 * (e % 2));
+      }
+    }
+  };
+  // Chunk j of the slice in r into a slot: X widened, dY as it is.
+  auto write_x = [&](const Set& r, int j, uint32_t slot) {
+    const float s = scale_of(r.s[j] >> xshift[j] & 255u);
+    u32x4_t lo, hi;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const u32x2_t p = widen4<F>(r.x[j][e], s), q = widen4<F>(r.x[j][2 + e], s);
+      lo[2 * e] = p[0];
+      lo[2 * e + 1] = p[1];
+      hi[2 * e] = q[0];
+      hi[2 * e + 1] = q[1];
+    }
+    typedef __attribute__((address_space(3))) u32x4_t lds_u32x4_t;
+    lds_u32x4_t* at = (lds_u32x4_t*)(uintptr_t)(xlds[j] + slot);
+    at[0] = lo;
+    at[1] = hi;
+  };
+  auto write_y = [&](const Set& r, int j, uint32_t slot) {
+    typedef __attribute__((address_space(3))) u32x4_t lds_u32x4_t;
+    *(lds_u32x4_t*)(uintptr_t)(ylds[j] + slot) = r.y[j];
+  };
+
+  f32x16_t acc[TM][TN];
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int j = 0; j < TN; ++j) acc[i][j] = f32x16_t{};
+
+  constexpr int NF = TM + TN, NM = TM * TN, NR = 2 * NF;
+  // Lane addresses of fragment f: 16 columns of 4 tokens per 16 lanes.
+  uint32_t fa[NF];
+#pragma unroll
+  for (int f = 0; f < NF; ++f) {
+    const int si = lane & 15, g = lane >> 4;
+    const int col = (f < TM ? wm * 32 * TM + 32 * f : wn * 32 * TN + 32 * (f - TM)) + 16 * (g & 1) + 4 * (si & 3);
+    const int kr = 8 * (g >> 1) + (si >> 2);
+    fa[f] = lds_addr(lds) + (f < TM ? kr * XP : KT * XP + kr * YP) + (((col >> 3) ^ row_swz(kr)) << 4) + 8 * (si & 1);
+  }
+  // Fragments of one step of 16 tokens, as halves until their wait.
+  u32x2_t half[2][NF][2];
+  u32x4_t fr[2][NF];
+  auto read_half = [&](auto o, auto step, auto slot, u32x2_t (&h)[NF][2]) {
+    constexpr int f = o / 2, r = o % 2;
+    constexpr int off = slot * STAGE + (16 * step + 4 * r) * (f < TM ? XP : YP);
+    h[f][r] = lds_read8_tr<off>(fa[f]);
+  };
+  auto landed = [&](u32x2_t (&h)[NF][2], u32x4_t (&to)[NF]) {
+    lgkm_wait();
+#pragma unroll
+    for (int f = 0; f < NF; ++f) {
+      hold(h[f][0]);
+      hold(h[f][1]);
+      to[f] = __builtin_shufflevector(h[f][0], h[f][1], 0, 1, 2, 3);
+    }
+  };
+  auto mfma = [&](const u32x4_t (&f)[NF], int q) {
+    const int i = q / TN, j = q % TN;
+    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, f[TM + j]),
+                                                        __builtin_bit_cast(bf16x8_t, f[i]), acc[i][j], 0, 0, 0);
+  };
+  using Zero = std::integral_constant<int, 0>;
+  using One = std::integral_constant<int, 1>;
+
+  if (count > 0) {
+    load_any(in[0], ke - 1);
+    if (count > 1) load_any(in[1], ke - 2);
+#pragma unroll
+    for (int j = 0; j < XC; ++j) write_x(in[0], j, 0);
+#pragma unroll
+    for (int j = 0; j < YC; ++j) write_y(in[0], j, 0);
+    if (count > 2) load_inner(in[0], kb);
+    lgkm_wait();
+    barrier_no_fence();
+    each<NR>([&](auto o) { read_half(o, Zero{}, Zero{}, half[0]); });
+    landed(half[0], fr[0]);
+  }
+  // The n-th slice, in slot P: its step 0 is in fr[0].  in[P ^ 1] holds the next.
+  auto slice = [&](auto set, auto more, int n) {
+    constexpr int P = decltype(set)::value;
+    using Here = std::integral_constant<int, P>;
+    using Next = std::integral_constant<int, P ^ 1>;
+    // Step 0, with the reads of step 1 and the next slice on its way to LDS (its
+    // slot was last read before the barrier of the slice before).
+    each<NM>([&](auto q) {
+      mfma(fr[0], q);
+      each<NR>([&](auto o) {
+        if constexpr (o >= q * NR / NM && o < (q + 1) * NR / NM) read_half(o, One{}, Here{}, half[1]);
+      });
+      each<XC + YC>([&](auto o) {
+        if constexpr (o >= q * (XC + YC) / NM && o < (q + 1) * (XC + YC) / NM) {
+          if constexpr (o < XC)
+            write_x(in[P ^ 1], o, Next::value * STAGE);
+          else
+            write_y(in[P ^ 1], o - XC, Next::value * STAGE);
+        }
+      });
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    landed(half[1], fr[1]);
+    mfma(fr[1], 0);
+    __builtin_amdgcn_sched_barrier(0);
+    barrier_no_fence();
+    each<NM - 1>([&](auto at) {
+      mfma(fr[1], at + 1);
+      constexpr int R = NM - 1;
+      each<NR>([&](auto o) {
+        if constexpr (o >= at * NR / R && o < (at + 1) * NR / R) read_half(o, Zero{}, Next{}, half[0]);
+      });
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    // The slice three on (past the end: the last, never used).
+    if constexpr (decltype(more)::value) load_inner(in[P ^ 1], kb + min(n + 3, count - 1) - 2);
+    landed(half[0], fr[0]);
+  };
+  using More = std::true_type;
+  using Few = std::false_type;
+  if (count > 2) {
+    int n = 0;
+    for (; n + 1 < count; n += 2) {
+      slice(Zero{}, More{}, n);
+      slice(One{}, More{}, n + 1);
+    }
+    if (n < count) slice(Zero{}, Few{}, n);
+  } else if (count > 0) {
+    slice(Zero{}, Few{}, 0);
+    if (count > 1) slice(One{}, Few{}, 1);
+  }
+  if (parts > 1 && !join_parts<TM, TN, W>(acc, split, t.ti * wide + t.tj, t.part, parts, wave, lane, &last)) return;
+  __syncthreads();
+  store_tile<T, TM, TN>(acc, reinterpret_cast<float*>(lds) + wave * 32 * (32 * TN + 4), dw, i0 + wm * 32 * TM,
+                        o0 + wn * 32 * TN, accumulate);
+}
+
+// A tile shape's cost in us, measured on 256 CUs: starting and storing a tile,
+// one slice of its long axis where a CU has one tile (of several, where tiles fill
+// the chip: the matrix cores then clock down), and joining `p` parts.
+struct TileCost {
+  int bm, bn;
+  double start, slice, slice_full, join, join_part;
+  double us(int64_t rows, int64_t cols, int64_t slices, int parts, int cus) const {
+    const int64_t groups = (rows + bm - 1) / bm * ((cols + bn - 1) / bn) * parts;
+    const double full = double(groups) / cus < 1.0 ? double(groups) / cus : 1.0;
+    const double each = start + (slice + (slice_full - slice) * full) * double((slices + parts - 1) / parts);
+    return double((groups + cus - 1) / cus) * each + (parts > 1 ? join + join_part * parts : 0.0);
+  }
+};
+
+struct Choice {
+  int tile = 0, parts = 1;
+};
+
+// The tile shape and the parts of the long axis that cost least.
+template <int N>
+Choice choose(const TileCost (&tiles)[N], int64_t rows, int64_t cols, int64_t slices, const SplitSpace& split,
+              int cus) {
+  Choice best;
+  double least = -1.0;
+  for (int t = 0; t < N; ++t) {
+    const int64_t count = (rows + tiles[t].bm - 1) / tiles[t].bm * ((cols + tiles[t].bn - 1) / tiles[t].bn);
+    for (int parts = 1; parts <= kMaxParts && parts <= slices; ++parts) {
+      if (parts > 1 && (count > kSplitCounts || count * parts * tiles[t].bm * tiles[t].bn > split.sum_floats)) break;
+      const double us = tiles[t].us(rows, cols, slices, parts, cus);
+      if (least < 0.0 || us < least) {
+        least = us;
+        best = Choice{t, parts};
+      }
+    }
+  }
+  return best;
+}
+
+template <typename F>
+void with_fp8(Fp8 v, F&& f) {
+  if (v == Fp8::E4M3)
+    f(std::integral_constant<Fp8, Fp8::E4M3>{});
+  else
+    f(std::integral_constant<Fp8, Fp8::E5M2>{});
 }
 
 }  // namespace
 
+// bf16 results: slices of 64 columns in 8 bits.  fp32 results: half the rate, so
+// the 256 x 256 tile, whose widened fragments do not fit its registers, is left
+// out.
+constexpr TileCost kProductTiles[] = {{256, 256, 9.0, 0.50, 0.80, 0.0, 5.5},
+                                      {128, 128, 3.0, 0.27, 0.28, 2.0, 0.8},
+                                      {64, 128, 1.0, 0.18, 0.20, 1.2, 0.6}};
+constexpr TileCost kProductExactTiles[] = {{128, 128, 3.5, 0.37, 0.43, 2.0, 0.8}, {64, 128, 1.0, 0.27, 0.29, 1.2, 0.6}};
+
 hipError_t launch_product(DType out_t, Fp8 a_fmt, const BlocksRef& a, const BlocksRef& b, const DenseRef& c,
-                          bool accumulate, const SplitSpace&, int, hipStream_t s) {
-  const unsigned tiles = unsigned((c.rows + 63) / 64 * ((c.cols + 63) / 64));
-  auto go = [&](auto k) { k<<<tiles, kThreads, 0, s>>>(a, b, c, accumulate); };
-  if (out_t == DType::BF16)
-    a_fmt == Fp8::E4M3 ? go(k_product<bf16, Fp8::E4M3>) : go(k_product<bf16, Fp8::E5M2>);
-  else
-    a_fmt == Fp8::E4M3 ? go(k_product<float, Fp8::E4M3>) : go(k_product<float, Fp8::E5M2>);
+                          bool accumulate, const SplitSpace& split, int cus, hipStream_t s) {
+  with_fp8(a_fmt, [&](auto fmt) {
+    constexpr Fp8 F = decltype(fmt)::value;
+    if (c.rows <= kFewRows) {
+      const unsigned groups = unsigned((a.cols + kGroupCols - 1) / kGroupCols);
+      const unsigned waves = groups < unsigned(kFewWaves) ? groups : unsigned(kFewWaves);
+      const unsigned tiles = unsigned((c.cols + 15) / 16);
+      if (out_t == DType::BF16)
+        k_product_few<bf16, F><<<tiles, 64 * waves, 0, s>>>(a, b, c, accumulate);
+      else
+        k_product_few<float, F><<<tiles, 64 * waves, 0, s>>>(a, b, c, accumulate);
+      return;
+    }
+    const int64_t blocks = (a.cols + kBlockCols - 1) / kBlockCols;
+    auto go = [&](auto k, const TileCost& t, int threads, int parts) {
+      const int64_t tiles = (c.rows + t.bm - 1) / t.bm * ((c.cols + t.bn - 1) / t.bn);
+      k<<<unsigned(tiles * parts), threads, 0, s>>>(a, b, c, accumulate, parts, split);
+    };
+    if (out_t == DType::BF16) {
+      const Choice p = choose(kProductTiles, c.rows, c.cols, 2 * blocks, split, cus);
+      const int parts = p.parts <= blocks ? p.parts : int(blocks);
+      if (p.tile == 0) return go(k_product<bf16, F, 4, 2, 2, 4>, kProductTiles[0], 512, parts);
+      if (p.tile == 1) return go(k_product<bf16, F, 2, 2, 2, 2>, kProductTiles[1], 256, parts);
+      return go(k_product<bf16, F, 1, 2, 2, 2>, kProductTiles[2], 256, parts);
+    }
+    const Choice p = choose(kProductExactTiles, c.rows, c.cols, 2 * blocks, split, cus);
+    const int parts = p.parts <= blocks ? p.parts : int(blocks);
+    if (p.tile == 0) return go(k_product<float, F, 2, 2, 2, 2>, kProductExactTiles[0], 256, parts);
+    return go(k_product<float, F, 1, 2, 2, 2>, kProductExactTiles[1], 256, parts);
+  });
   return hipGetLastError();
 }
 
+// Slices of 32 tokens.
+constexpr TileCost kWeightGradTiles[] = {{256, 256, 9.0, 0.64, 0.84, 0.0, 6.3}, {128, 128, 5.0, 0.34, 0.30, 2.0, 0.9}};
+
 hipError_t launch_weight_grad(DType out_t, Fp8 x_fmt, const BlocksRef& x, const DenseRef& dy, const DenseRef& dw,
-                              bool accumulate, const SplitSpace&, int, hipStream_t s) {
-  const unsigned tiles = unsigned((dw.rows + 63) / 64 * ((dw.cols + 63) / 64));
-  auto go = [&](auto k) { k<<<tiles, kThreads, 0, s>>>(x, dy, dw, accumulate); };
-  if (out_t == DType::BF16)
-    x_fmt == Fp8::E4M3 ? go(k_weight_grad<bf16, Fp8::E4M3>) : go(k_weight_grad<bf16, Fp8::E5M2>);
-  else
-    x_fmt == Fp8::E4M3 ? go(k_weight_grad<float, Fp8::E4M3>) : go(k_weight_grad<float, Fp8::E5M2>);
+                              bool accumulate, const SplitSpace& split, int cus, hipStream_t s) {
+  const Choice p = choose(kWeightGradTiles, dw.rows, dw.cols, (x.rows + 31) / 32, split, cus);
+  with_fp8(x_fmt, [&](auto fmt) {
+    constexpr Fp8 F = decltype(fmt)::value;
+    auto go = [&](auto k, int threads) {
+      const TileCost& t = kWeightGradTiles[p.tile];
+      const int64_t tiles = (dw.rows + t.bm - 1) / t.bm * ((dw.cols + t.bn - 1) / t.bn);
+      k<<<unsigned(tiles * p.parts), threads, 0, s>>>(x, dy, dw, accumulate, p.parts, split);
+    };
+    if (out_t == DType::BF16)
+      p.tile == 0 ? go(k_weight_grad<bf16, F, 4, 2, 2, 4>, 512) : go(k_weight_grad<bf16, F, 2, 2, 2, 2>, 256);
+    else
+      p.tile == 0 ? go(k_weight_grad<float, F, 4, 2, 2, 4>, 512) : go(k_weight_grad<float, F, 2, 2, 2, 2>, 256);
+  });
   return hipGetLastError();
 }
 
