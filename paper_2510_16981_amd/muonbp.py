@@ -481,25 +481,53 @@ class Blocks:
     (cols rounded up to 128 at least), ``scales`` int32, ceil(cols / 512) x
     rows, a byte for each block.  Holds its tensors; makes no copy."""
 
-    __slots__ = ("data", "scales", "rows", "cols", "format", "ref", "addr")
+    __slots__ = ("_data", "_scales", "_memory", "rows", "cols", "format", "device", "ref", "addr")
 
     def __init__(self, data, scales, cols: int, format: int = E4M3):
         import torch
-        rows = data.shape[0]
+        rows, width = data.shape
         groups = -(-cols // GROUP_COLS)
-        if not (data.dim() == 2 and data.dtype == torch.uint8 and data.is_cuda and data.stride(1) == 1
-                and data.shape[1] >= -(-cols // BLOCK_COLS) * BLOCK_COLS):
+        if not (data.dtype is torch.uint8 and data.is_cuda and data.stride(1) == 1
+                and width >= -(-cols // BLOCK_COLS) * BLOCK_COLS):
             raise ValueError(f"data: need a CUDA uint8 matrix with rows of at least {cols} bytes rounded up "
                              f"to {BLOCK_COLS}, got {data.dtype} {tuple(data.shape)}")
-        if not (tuple(scales.shape) == (groups, rows) and scales.dtype == torch.int32
+        if not (scales.shape == (groups, rows) and scales.dtype is torch.int32
                 and scales.device == data.device and (rows <= 1 or scales.stride(1) == 1)):
             raise ValueError(f"scales: need an int32 matrix of shape {(groups, rows)} on {data.device}, "
                              f"got {scales.dtype} {tuple(scales.shape)}")
-        self.data, self.scales, self.rows, self.cols, self.format = data, scales, rows, int(cols), int(format)
-        self.ref = BlocksRef(data.data_ptr(), scales.data_ptr(), rows, cols,
-                             data.stride(0) if rows > 1 else data.shape[1],
-                             scales.stride(0) if groups > 1 else rows, format)
+        self._data, self._scales, self._memory = data, scales, None
+        self._describe(data.data_ptr(), scales.data_ptr(), rows, cols, data.stride(0) if rows > 1 else width,
+                       scales.stride(0) if groups > 1 else rows, format, data.device)
+
+    def _describe(self, data, scales, rows, cols, ld, scale_ld, format, device):
+        self.rows, self.cols, self.format, self.device = rows, cols, format, device
+        self.ref = BlocksRef(data, scales, rows, cols, ld, scale_ld, format)
         self.addr = ctypes.addressof(self.ref)
+
+    @classmethod
+    def _in(cls, memory, rows: int, cols: int, ld: int, format: int) -> "Blocks":
+        """Blocks in one uint8 tensor: rows x ld bytes, then the scales."""
+        self = object.__new__(cls)
+        self._data = self._scales = None
+        self._memory = memory
+        at = memory.data_ptr()
+        self._describe(at, at + rows * ld, rows, cols, ld, rows, format, memory.device)
+        return self
+
+    @property
+    def data(self):
+        if self._data is None:
+            rows, ld = self.rows, self.ref.ld
+            self._data = self._memory[:rows * ld].view(rows, ld)
+        return self._data
+
+    @property
+    def scales(self):
+        if self._scales is None:
+            import torch
+            rows, ld = self.rows, self.ref.ld
+            self._scales = self._memory[rows * ld:].view(torch.int32).view(-(-self.cols // GROUP_COLS), rows)
+        return self._scales
 
     def __getitem__(self, rows: slice) -> "Blocks":
         """Rows [a, b) as a matrix of the same memory."""
@@ -535,6 +563,10 @@ class Linear:
         self.device = stream.device
         self._torch = torch
         self._codes = {torch.float32: F32, torch.bfloat16: BF16}
+        # The handle of the current stream: torch.cuda.current_stream builds an
+        # object for it, which takes longer than the rest of a call.
+        self._current = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+            lambda index: torch.cuda.current_stream(index).cuda_stream)
 
     # -- helpers
     def _check(self, st: int, what: str):
@@ -554,22 +586,22 @@ class Linear:
         return Dense(t.data_ptr(), rows, cols, ld if rows > 1 else cols, code)
 
     def _blocks(self, b: Blocks, name: str):
-        if not isinstance(b, Blocks) or b.data.device != self.device:
+        if not isinstance(b, Blocks) or b.device != self.device:
             raise ValueError(f"{name}: need Blocks on {self.device}")
         return b.addr
 
-    def _empty(self, rows: int, cols: int, dtype):
+    def _empty(self, shape, dtype):
         torch = self._torch
-        if torch.cuda.current_stream(self.device) == self._stream:
-            return torch.empty((rows, cols), dtype=dtype, device=self.device)
+        if self._current(self.device.index) == self._stream.cuda_stream:
+            return torch.empty(shape, dtype=dtype, device=self.device)
         with torch.cuda.stream(self._stream):
-            return torch.empty((rows, cols), dtype=dtype, device=self.device)
+            return torch.empty(shape, dtype=dtype, device=self.device)
 
     def empty_blocks(self, rows: int, cols: int, format: int = E4M3) -> Blocks:
         """Uninitialised Blocks of rows x cols."""
-        torch = self._torch
-        return Blocks(self._empty(rows, -(-cols // BLOCK_COLS) * BLOCK_COLS, torch.uint8),
-                      self._empty(-(-cols // GROUP_COLS), rows, torch.int32), cols, format)
+        ld = -(-cols // BLOCK_COLS) * BLOCK_COLS
+        return Blocks._in(self._empty(rows * (ld + 4 * -(-cols // GROUP_COLS)), self._torch.uint8), rows, cols, ld,
+                          format)
 
     # -- API
     def quantize(self, x, format: int = E4M3, out: Optional[Blocks] = None) -> Blocks:
@@ -598,7 +630,7 @@ class Linear:
         """The values of x (bf16 by default), exact."""
         a = self._blocks(x, "x")
         if out is None:
-            out = self._empty(x.rows, x.cols, dtype or self._torch.bfloat16)
+            out = self._empty((x.rows, x.cols), dtype or self._torch.bfloat16)
         d = self._dense(out, "out")
         self._check(self.lib.muonbp_linear_restore(self.ctx, a, ctypes.addressof(d)), "restore")
         return out
@@ -609,7 +641,7 @@ class Linear:
         if out is None:
             if accumulate:
                 raise ValueError("accumulate needs out")
-            out = self._empty(a.rows, b.rows, dtype or self._torch.bfloat16)
+            out = self._empty((a.rows, b.rows), dtype or self._torch.bfloat16)
         d = self._dense(out, "out")
         self._check(self.lib.muonbp_linear_product(self.ctx, pa, pb, ctypes.addressof(d), int(accumulate)),
                     "product")
@@ -621,7 +653,7 @@ class Linear:
         if out is None:
             if accumulate:
                 raise ValueError("accumulate needs out")
-            out = self._empty(x.cols, dd.cols, dtype or self._torch.bfloat16)
+            out = self._empty((x.cols, dd.cols), dtype or self._torch.bfloat16)
         d = self._dense(out, "out")
         self._check(self.lib.muonbp_linear_weight_grad(self.ctx, px, ctypes.addressof(dd), ctypes.addressof(d),
                                                        int(accumulate)), "weight_grad")
@@ -631,7 +663,7 @@ class Linear:
         """(h, gate, up) with h = silu(gate) up of the inputs' dtype (``blocks``:
         in 8 bits) and gate and up kept in 8 bits (None without ``keep``)."""
         g, u = self._dense(gate, "gate"), self._dense(up, "up")
-        h = self.empty_blocks(g.rows, g.cols, format) if blocks else self._empty(g.rows, g.cols, gate.dtype)
+        h = self.empty_blocks(g.rows, g.cols, format) if blocks else self._empty((g.rows, g.cols), gate.dtype)
         dense = None if blocks else self._dense(h, "h")
         g8, u8 = (self.empty_blocks(g.rows, g.cols, format) if keep else None for _ in range(2))
         self._check(self.lib.muonbp_linear_gated_forward(
@@ -643,7 +675,7 @@ class Linear:
         """(dgate, dup) of dh's dtype, and with ``blocks`` both in 8 bits too."""
         d = self._dense(dh, "dh")
         pg, pu = self._blocks(gate, "gate"), self._blocks(up, "up")
-        dgate, dup = (self._empty(d.rows, d.cols, dh.dtype) for _ in range(2))
+        dgate, dup = (self._empty((d.rows, d.cols), dh.dtype) for _ in range(2))
         a, b = self._dense(dgate, "dgate"), self._dense(dup, "dup")
         dgate8, dup8 = (self.empty_blocks(d.rows, d.cols, format) if blocks else None for _ in range(2))
         self._check(self.lib.muonbp_linear_gated_backward(
