@@ -92,6 +92,8 @@ __device__ __forceinline__ void store_tile(f32x16_t (&acc)[TM][TN], float* st, c
   constexpr int P = 32 * TN + 4;
   constexpr int CH = 4 * TN;  // 8-element chunks of a row
   const int lane = threadIdx.x & 63;
+  // Inside the matrix: stores without tests between them.
+  const bool whole = !accumulate && row0 + 32 * TM <= c.rows && col0 + 32 * TN <= c.cols;
 #pragma unroll
   for (int i = 0; i < TM; ++i) {
 #pragma unroll
@@ -100,6 +102,17 @@ __device__ __forceinline__ void store_tile(f32x16_t (&acc)[TM][TN], float* st, c
       for (int q = 0; q < 4; ++q)
         *reinterpret_cast<f32x4_t*>(st + (lane & 31) * P + 32 * j + 8 * q + 4 * (lane >> 5)) =
             f32x4_t{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+    if (whole) {
+#pragma unroll
+      for (int p = 0; p < 32 * CH / 64; ++p) {
+        const int at = p * 64 + lane, r = at / CH, k = 8 * (at % CH);
+        float f[8];
+        *reinterpret_cast<f32x4_t*>(f) = *reinterpret_cast<const f32x4_t*>(st + r * P + k);
+        *reinterpret_cast<f32x4_t*>(f + 4) = *reinterpret_cast<const f32x4_t*>(st + r * P + k + 4);
+        store8(static_cast<T*>(c.ptr) + (row0 + 32 * i + r) * c.ld + col0 + k, 8, f);
+      }
+      continue;
+    }
 #pragma unroll
     for (int p = 0; p < 32 * CH / 64; ++p) {
       const int at = p * 64 + lane, r = at / CH, k = 8 * (at % CH);
@@ -578,11 +591,14 @@ __global__ __launch_bounds__(64 * WM * WN) void k_weight_grad(BlocksRef x, Dense
   const uint32_t* const sbase = x.scales + i0 / kGroupCols * x.scale_ld;
   const uint16_t* const ybase = static_cast<const uint16_t*>(dy.ptr) + o0;
 
+  constexpr int NF = TM + TN, NM = TM * TN, NR = 2 * NF;
   struct Set {
     u32x4_t x[XC], y[YC];
     uint32_t s[XC];
   };
-  Set in[2];
+  // Slices on their way: a small tile's take less time than a load from memory.
+  constexpr int SETS = NM <= 4 ? 4 : 2;
+  Set in[SETS];
   // Slice k: at least 8 tokens follow it, so a 16-byte load that passes the end
   // of its row stays inside the matrix.
   auto load_inner = [&](Set& r, int64_t k) {
@@ -596,28 +612,34 @@ __global__ __launch_bounds__(64 * WM * WN) void k_weight_grad(BlocksRef x, Dense
     for (int j = 0; j < YC; ++j)
       r.y[j] = gload<u32x4_t, 2>(reinterpret_cast<const unsigned char*>(ybase + t0 * dy.ld) + yoff[j]);
   };
+  // Any slice: tokens past the end as zeros, and where 16 bytes would pass the
+  // end of a row, its elements one by one.
   auto load_any = [&](Set& r, int64_t k) {
     const int64_t t0 = k * KT;
     if (t0 + KT + 8 <= tokens) return load_inner(r, k);
 #pragma unroll
     for (int j = 0; j < XC; ++j) {
-      r.x[j] = u32x4_t{0, 0, 0, 0};
-      r.s[j] = 0;
-      if (t0 + xt[j] < tokens) {
-        r.x[j] = gload<u32x4_t, 16>(xbase + t0 * x.ld + xoff[j]);
-        r.s[j] = gload<uint32_t, 4>(sbase + t0 + xt[j]);
-      }
+      const int64_t row = t0 + xt[j];
+      const int64_t at = row < tokens ? 0 : tokens - 1 - row;  // back to the last token
+      r.x[j] = gload<u32x4_t, 16>(xbase + t0 * x.ld + at * x.ld + xoff[j]);
+      r.s[j] = gload<uint32_t, 4>(sbase + row + at);
+      if (at) r.x[j] = u32x4_t{0, 0, 0, 0};
     }
 #pragma unroll
     for (int j = 0; j < YC; ++j) {
-      r.y[j] = u32x4_t{0, 0, 0, 0};
-      if (t0 + yt[j] < tokens) {
-        const uint16_t* p = ybase + (t0 + yt[j]) * dy.ld + ycol[j];
-        const int64_t n = dy.cols - o0 - ycol[j];
+      const int64_t row = t0 + yt[j];
+      const uint16_t* p = ybase + (row < tokens ? row : tokens - 1) * dy.ld + ycol[j];
+      const int64_t n = dy.cols - o0 - ycol[j];
+      if (n >= 8) {
+        r.y[j] = gload<u32x4_t, 2>(p);
+      } else {
+        uint32_t h[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (e < n) r.y[j][e / 2] |= uint32_t(gload<uint16_t, 2>(p + e)) << (16 * (e % 2));
+        for (int e = 0; e < 8; ++e) h[e] = gload<uint16_t, 2>(p + (e < n ? e : 0));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) r.y[j][e] = h[2 * e] | h[2 * e + 1] << 16;
       }
+      if (row >= tokens) r.y[j] = u32x4_t{0, 0, 0, 0};
     }
   };
   // Chunk j of the slice in r into a slot: X widened, dY as it is.
@@ -648,7 +670,6 @@ __global__ __launch_bounds__(64 * WM * WN) void k_weight_grad(BlocksRef x, Dense
 #pragma unroll
     for (int j = 0; j < TN; ++j) acc[i][j] = f32x16_t{};
 
-  constexpr int NF = TM + TN, NM = TM * TN, NR = 2 * NF;
   // Lane addresses of fragment f: 16 columns of 4 tokens per 16 lanes.
   uint32_t fa[NF];
 #pragma unroll
@@ -659,14 +680,14 @@ __global__ __launch_bounds__(64 * WM * WN) void k_weight_grad(BlocksRef x, Dense
     fa[f] = lds_addr(lds) + (f < TM ? kr * XP : KT * XP + kr * YP) + (((col >> 3) ^ row_swz(kr)) << 4) + 8 * (si & 1);
   }
   // Fragments of one step of 16 tokens, as halves until their wait.
-  u32x2_t half[2][NF][2];
-  u32x4_t fr[2][NF];
-  auto read_half = [&](auto o, auto step, auto slot, u32x2_t (&h)[NF][2]) {
+  using Half = u32x2_t[NF][2];
+  using Frag = u32x4_t[NF];
+  auto read_half = [&](auto o, auto step, auto slot, Half& h) {
     constexpr int f = o / 2, r = o % 2;
     constexpr int off = slot * STAGE + (16 * step + 4 * r) * (f < TM ? XP : YP);
     h[f][r] = lds_read8_tr<off>(fa[f]);
   };
-  auto landed = [&](u32x2_t (&h)[NF][2], u32x4_t (&to)[NF]) {
+  auto landed = [&](Half& h, Frag& to) {
     lgkm_wait();
 #pragma unroll
     for (int f = 0; f < NF; ++f) {
@@ -675,46 +696,52 @@ __global__ __launch_bounds__(64 * WM * WN) void k_weight_grad(BlocksRef x, Dense
       to[f] = __builtin_shufflevector(h[f][0], h[f][1], 0, 1, 2, 3);
     }
   };
-  auto mfma = [&](const u32x4_t (&f)[NF], int q) {
+  auto mfma = [&](const Frag& f, int q) {
     const int i = q / TN, j = q % TN;
     acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, f[TM + j]),
                                                         __builtin_bit_cast(bf16x8_t, f[i]), acc[i][j], 0, 0, 0);
   };
+  // Write o of slice r into a slot.
+  auto write = [&](auto o, const Set& r, uint32_t slot) {
+    if constexpr (o < XC)
+      write_x(r, o, slot);
+    else
+      write_y(r, o - XC, slot);
+  };
   using Zero = std::integral_constant<int, 0>;
   using One = std::integral_constant<int, 1>;
-
+  constexpr int NW = XC + YC;
+  // The n-th slice, n >= 2 (past the end: the last, unused).
+  auto load_next = [&](Set& r, int n) { load_inner(r, kb + min(n, count - 1) - 2); };
+  Half half[2];
+  Frag fr[2];
   if (count > 0) {
     load_any(in[0], ke - 1);
     if (count > 1) load_any(in[1], ke - 2);
-#pragma unroll
-    for (int j = 0; j < XC; ++j) write_x(in[0], j, 0);
-#pragma unroll
-    for (int j = 0; j < YC; ++j) write_y(in[0], j, 0);
-    if (count > 2) load_inner(in[0], kb);
+    if (count > 2)
+      each<SETS - 2>([&](auto i) { load_next(in[i + 2], i + 2); });
+    each<NW>([&](auto o) { write(o, in[0], 0); });
+    if (count > 2) load_next(in[0], SETS);
     lgkm_wait();
     barrier_no_fence();
     each<NR>([&](auto o) { read_half(o, Zero{}, Zero{}, half[0]); });
     landed(half[0], fr[0]);
   }
-  // The n-th slice, in slot P: its step 0 is in fr[0].  in[P ^ 1] holds the next.
-  auto slice = [&](auto set, auto more, int n) {
-    constexpr int P = decltype(set)::value;
+  // Slice n, n % SETS = i, in slot n % 2, its step 0 in fr[0]; the next SETS - 1
+  // slices are in registers or on their way there.
+  auto slice = [&](auto i, auto more, int n) {
+    constexpr int P = i % 2, Q = P ^ 1, S = (i + 1) % SETS;
     using Here = std::integral_constant<int, P>;
-    using Next = std::integral_constant<int, P ^ 1>;
-    // Step 0, with the reads of step 1 and the next slice on its way to LDS (its
-    // slot was last read before the barrier of the slice before).
+    using Next = std::integral_constant<int, Q>;
+    // Step 0, with the reads of step 1 and the next slice on its way to LDS
+    // (its slot was last read before the barrier of the slice before).
     each<NM>([&](auto q) {
       mfma(fr[0], q);
       each<NR>([&](auto o) {
         if constexpr (o >= q * NR / NM && o < (q + 1) * NR / NM) read_half(o, One{}, Here{}, half[1]);
       });
-      each<XC + YC>([&](auto o) {
-        if constexpr (o >= q * (XC + YC) / NM && o < (q + 1) * (XC + YC) / NM) {
-          if constexpr (o < XC)
-            write_x(in[P ^ 1], o, Next::value * STAGE);
-          else
-            write_y(in[P ^ 1], o - XC, Next::value * STAGE);
-        }
+      each<NW>([&](auto o) {
+        if constexpr (o >= q * NW / NM && o < (q + 1) * NW / NM) write(o, in[S], Q * STAGE);
       });
       __builtin_amdgcn_sched_barrier(0);
     });
@@ -722,30 +749,26 @@ __global__ __launch_bounds__(64 * WM * WN) void k_weight_grad(BlocksRef x, Dense
     mfma(fr[1], 0);
     __builtin_amdgcn_sched_barrier(0);
     barrier_no_fence();
-    each<NM - 1>([&](auto at) {
+    constexpr int R = NM - 1;
+    each<R>([&](auto at) {
       mfma(fr[1], at + 1);
-      constexpr int R = NM - 1;
       each<NR>([&](auto o) {
         if constexpr (o >= at * NR / R && o < (at + 1) * NR / R) read_half(o, Zero{}, Next{}, half[0]);
       });
       __builtin_amdgcn_sched_barrier(0);
     });
-    // The slice three on (past the end: the last, never used).
-    if constexpr (decltype(more)::value) load_inner(in[P ^ 1], kb + min(n + 3, count - 1) - 2);
+    if constexpr (decltype(more)::value) load_next(in[S], n + 1 + SETS);
     landed(half[0], fr[0]);
   };
-  using More = std::true_type;
-  using Few = std::false_type;
+  int n = 0;
   if (count > 2) {
-    int n = 0;
-    for (; n + 1 < count; n += 2) {
-      slice(Zero{}, More{}, n);
-      slice(One{}, More{}, n + 1);
-    }
-    if (n < count) slice(Zero{}, Few{}, n);
-  } else if (count > 0) {
-    slice(Zero{}, Few{}, 0);
-    if (count > 1) slice(One{}, Few{}, 1);
+    for (; n + SETS <= count; n += SETS) each<SETS>([&](auto i) { slice(i, std::true_type{}, n + i); });
+    each<SETS - 1>([&](auto i) {
+      if (n + i < count) slice(i, std::false_type{}, n + i);
+    });
+  } else {
+    if (count > 0) slice(Zero{}, std::false_type{}, 0);
+    if (count > 1) slice(One{}, std::false_type{}, 1);
   }
   if (parts > 1 && !join_parts<TM, TN, W>(acc, split, t.ti * wide + t.tj, t.part, parts, wave, lane, &last)) return;
   __syncthreads();
@@ -754,16 +777,20 @@ __global__ __launch_bounds__(64 * WM * WN) void k_weight_grad(BlocksRef x, Dense
 }
 
 // A tile shape's cost in us, measured on 256 CUs: starting and storing a tile,
-// one slice of its long axis where a CU has one tile (of several, where tiles fill
-// the chip: the matrix cores then clock down), and joining `p` parts.
+// and one slice of its long axis where a CU has one tile, or `full` of them or
+// more (slower where the matrix cores then clock down, faster where tiles hide
+// each other's waits).  Joining parts writes and reads all their sums, at 5 TB/s.
 struct TileCost {
   int bm, bn;
-  double start, slice, slice_full, join, join_part;
+  double start, slice, slice_full;
+  int full;
   double us(int64_t rows, int64_t cols, int64_t slices, int parts, int cus) const {
     const int64_t groups = (rows + bm - 1) / bm * ((cols + bn - 1) / bn) * parts;
-    const double full = double(groups) / cus < 1.0 ? double(groups) / cus : 1.0;
-    const double each = start + (slice + (slice_full - slice) * full) * double((slices + parts - 1) / parts);
-    return double((groups + cus - 1) / cus) * each + (parts > 1 ? join + join_part * parts : 0.0);
+    const double load = double(groups) / cus - (full - 1);
+    const double at = load < 0.0 ? 0.0 : load > 1.0 ? 1.0 : load;
+    const double each = start + (slice + (slice_full - slice) * at) * double((slices + parts - 1) / parts);
+    const double join = parts > 1 ? 1.0 + 0.4 * parts + 8.0 * double(groups) * bm * bn / 5e6 : 0.0;
+    return double((groups + cus - 1) / cus) * each + join;
   }
 };
 
@@ -804,10 +831,11 @@ void with_fp8(Fp8 v, F&& f) {
 // bf16 results: slices of 64 columns in 8 bits.  fp32 results: half the rate, so
 // the 256 x 256 tile, whose widened fragments do not fit its registers, is left
 // out.
-constexpr TileCost kProductTiles[] = {{256, 256, 9.0, 0.50, 0.80, 0.0, 5.5},
-                                      {128, 128, 3.0, 0.27, 0.28, 2.0, 0.8},
-                                      {64, 128, 1.0, 0.18, 0.20, 1.2, 0.6}};
-constexpr TileCost kProductExactTiles[] = {{128, 128, 3.5, 0.37, 0.43, 2.0, 0.8}, {64, 128, 1.0, 0.27, 0.29, 1.2, 0.6}};
+constexpr TileCost kProductTiles[] = {{256, 256, 8.0, 0.50, 0.78, 1},
+                                      {128, 128, 2.5, 0.25, 0.28, 2},
+                                      {64, 128, 1.0, 0.18, 0.20, 2},
+                                      {128, 256, 5.0, 0.32, 0.46, 1}};
+constexpr TileCost kProductExactTiles[] = {{128, 128, 3.0, 0.37, 0.43, 2}, {64, 128, 1.0, 0.27, 0.29, 2}};
 
 hipError_t launch_product(DType out_t, Fp8 a_fmt, const BlocksRef& a, const BlocksRef& b, const DenseRef& c,
                           bool accumulate, const SplitSpace& split, int cus, hipStream_t s) {
@@ -833,7 +861,8 @@ hipError_t launch_product(DType out_t, Fp8 a_fmt, const BlocksRef& a, const Bloc
       const int parts = p.parts <= blocks ? p.parts : int(blocks);
       if (p.tile == 0) return go(k_product<bf16, F, 4, 2, 2, 4>, kProductTiles[0], 512, parts);
       if (p.tile == 1) return go(k_product<bf16, F, 2, 2, 2, 2>, kProductTiles[1], 256, parts);
-      return go(k_product<bf16, F, 1, 2, 2, 2>, kProductTiles[2], 256, parts);
+      if (p.tile == 2) return go(k_product<bf16, F, 1, 2, 2, 2>, kProductTiles[2], 256, parts);
+      return go(k_product<bf16, F, 2, 2, 2, 4>, kProductTiles[3], 512, parts);
     }
     const Choice p = choose(kProductExactTiles, c.rows, c.cols, 2 * blocks, split, cus);
     const int parts = p.parts <= blocks ? p.parts : int(blocks);
@@ -844,7 +873,7 @@ hipError_t launch_product(DType out_t, Fp8 a_fmt, const BlocksRef& a, const Bloc
 }
 
 // Slices of 32 tokens.
-constexpr TileCost kWeightGradTiles[] = {{256, 256, 9.0, 0.64, 0.84, 0.0, 6.3}, {128, 128, 5.0, 0.34, 0.30, 2.0, 0.9}};
+constexpr TileCost kWeightGradTiles[] = {{256, 256, 8.0, 0.64, 0.82, 1}, {128, 128, 4.0, 0.36, 0.29, 2}};
 
 hipError_t launch_weight_grad(DType out_t, Fp8 x_fmt, const BlocksRef& x, const DenseRef& dy, const DenseRef& dw,
                               bool accumulate, const SplitSpace& split, int cus, hipStream_t s) {
