@@ -61,20 +61,39 @@ __device__ __forceinline__ uint32_t lds_addr(const void* p) {
   return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((const lds_void_t*)p));
 }
 
-// Which tile workgroup b of a grid of tall x wide tiles x parts runs.  Consecutive
-// workgroups go to the 8 XCDs in turn; each XCD gets a contiguous run of tiles,
-// taken `kGroupTall` tiles high, so that the tiles resident on one XCD share
-// rows and columns in its L2.
+// How a grid of tall x wide tiles is shared out: the first `whole` tiles to one
+// workgroup each, the others, their long axis in `parts`, to `parts` workgroups
+// each.
+struct Shares {
+  int whole, parts;
+};
+
+// Which tile and part workgroup b runs.  Consecutive workgroups go to the 8 XCDs
+// in turn; each XCD gets a contiguous run of tiles, taken `kGroupTall` tiles
+// high, so that the tiles resident on one XCD share rows and columns in its L2.
 struct TileAt {
-  int ti, tj, part;
+  int ti, tj, part, parts;
+  int split;  // its place among the tiles in parts
 };
 constexpr int kXcds = 8, kGroupTall = 8;
-__device__ __forceinline__ TileAt tile_at(int b, int total, int tall, int wide, int parts) {
+__device__ __forceinline__ int spread(int b, int total) {
   const int x = b % kXcds, q = total / kXcds, r = total % kXcds;
-  int pos = x * q + min(x, r) + b / kXcds;
+  return x * q + min(x, r) + b / kXcds;
+}
+__device__ __forceinline__ TileAt tile_at(int b, int total, int tall, int wide, const Shares& s) {
   TileAt t;
-  t.part = pos % parts;
-  pos /= parts;
+  int pos;
+  if (b < s.whole) {
+    pos = spread(b, s.whole);
+    t.part = t.split = 0;
+    t.parts = 1;
+  } else {
+    const int at = spread(b - s.whole, total - s.whole);
+    t.split = at / s.parts;
+    t.part = at - t.split * s.parts;
+    t.parts = s.parts;
+    pos = s.whole + t.split;
+  }
   const int per = kGroupTall * wide, g = pos / per, in = pos - g * per;
   const int h = min(kGroupTall, tall - g * kGroupTall);
   t.ti = g * kGroupTall + in % h;
@@ -206,7 +225,7 @@ __device__ __forceinline__ int swz(int row) { return ((row >> 1) & 3) ^ ((row >>
 
 template <typename T, Fp8 F, int TM, int TN, int WM, int WN>
 __global__ __launch_bounds__(64 * WM * WN) void k_product(BlocksRef a, BlocksRef b, DenseRef c, bool accumulate,
-                                                          int parts, SplitSpace split) {
+                                                          Shares shares, SplitSpace split) {
   constexpr bool EXACT = sizeof(T) == 4;
   constexpr int BM = 32 * TM * WM, BN = 32 * TN * WN, W = WM * WN, NS = 4, ROW = 64;
   constexpr int STAGE = (BM + BN) * ROW;
@@ -221,7 +240,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_product(BlocksRef a, BlocksRef
   uint32_t* const words = reinterpret_cast<uint32_t*>(lds + RING);
 
   const int tall = int((c.rows + BM - 1) / BM), wide = int((c.cols + BN - 1) / BN);
-  const TileAt t = tile_at(blockIdx.x, gridDim.x, tall, wide, parts);
+  const TileAt t = tile_at(blockIdx.x, gridDim.x, tall, wide, shares);
   const int64_t m0 = int64_t(t.ti) * BM, n0 = int64_t(t.tj) * BN;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -234,7 +253,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_product(BlocksRef a, BlocksRef
 
   // Slices of this part: whole blocks of 128.
   const int nblk = int(kbytes / kBlockCols);
-  const int kb = 2 * int(int64_t(t.part) * nblk / parts), ke = 2 * int(int64_t(t.part + 1) * nblk / parts);
+  const int kb = 2 * int(int64_t(t.part) * nblk / t.parts), ke = 2 * int(int64_t(t.part + 1) * nblk / t.parts);
 
   uint32_t voff[LP];
 #pragma unroll
@@ -404,7 +423,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_product(BlocksRef a, BlocksRef
     for (int f = 0; f < NF; ++f) hold(sw[f]);
   }
   __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));  // copies past the end land before the ring is reused
-  if (parts > 1 && !join_parts<TM, TN, W>(acc, split, t.ti * wide + t.tj, t.part, parts, wave, lane, &last)) return;
+  if (t.parts > 1 && !join_parts<TM, TN, W>(acc, split, t.split, t.part, t.parts, wave, lane, &last)) return;
   __syncthreads();
   store_tile<T, TM, TN>(acc, reinterpret_cast<float*>(lds) + wave * 32 * (32 * TN + 4), c,
                         m0 + wm * 32 * TM, n0 + wn * 32 * TN, accumulate);
@@ -544,7 +563,7 @@ __device__ __forceinline__ u32x2_t lds_read8_tr(uint32_t addr) {
 
 template <typename T, Fp8 F, int TM, int TN, int WM, int WN>
 __global__ __launch_bounds__(64 * WM * WN) void k_weight_grad(BlocksRef x, DenseRef dy, DenseRef dw, bool accumulate,
-                                                              int parts, SplitSpace split) {
+                                                              Shares shares, SplitSpace split) {
   constexpr int BM = 32 * TM * WM, BN = 32 * TN * WN, W = WM * WN, NT = 64 * W, KT = 32;
   constexpr int XP = 2 * BM, YP = 2 * BN, STAGE = KT * (XP + YP);  // bytes
   constexpr int XC = KT * BM / 16 / NT, YC = KT * BN / 8 / NT;     // 16-byte loads per thread and slice
@@ -554,7 +573,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_weight_grad(BlocksRef x, Dense
   __shared__ int last;
 
   const int tall = int((dw.rows + BM - 1) / BM), wide = int((dw.cols + BN - 1) / BN);
-  const TileAt t = tile_at(blockIdx.x, gridDim.x, tall, wide, parts);
+  const TileAt t = tile_at(blockIdx.x, gridDim.x, tall, wide, shares);
   const int64_t i0 = int64_t(t.ti) * BM, o0 = int64_t(t.tj) * BN;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -562,7 +581,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_weight_grad(BlocksRef x, Dense
   // Slices of this part, in the order ke - 1, ke - 2, kb, kb + 1, ...
   const int64_t tokens = x.rows;
   const int64_t nk = (tokens + KT - 1) / KT;
-  const int64_t kb = t.part * nk / parts, ke = (t.part + 1) * nk / parts;
+  const int64_t kb = t.part * nk / t.parts, ke = (t.part + 1) * nk / t.parts;
   const int count = int(ke - kb);
 
   const int64_t padded = (x.cols + kBlockCols - 1) / kBlockCols * kBlockCols;
@@ -770,7 +789,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_weight_grad(BlocksRef x, Dense
     if (count > 0) slice(Zero{}, std::false_type{}, 0);
     if (count > 1) slice(One{}, std::false_type{}, 1);
   }
-  if (parts > 1 && !join_parts<TM, TN, W>(acc, split, t.ti * wide + t.tj, t.part, parts, wave, lane, &last)) return;
+  if (t.parts > 1 && !join_parts<TM, TN, W>(acc, split, t.split, t.part, t.parts, wave, lane, &last)) return;
   __syncthreads();
   store_tile<T, TM, TN>(acc, reinterpret_cast<float*>(lds) + wave * 32 * (32 * TN + 4), dw, i0 + wm * 32 * TM,
                         o0 + wn * 32 * TN, accumulate);
@@ -784,36 +803,49 @@ struct TileCost {
   int bm, bn;
   double start, slice, slice_full;
   int full;
-  double us(int64_t rows, int64_t cols, int64_t slices, int parts, int cus) const {
-    const int64_t groups = (rows + bm - 1) / bm * ((cols + bn - 1) / bn) * parts;
+  // Of `groups` workgroups that run `slices` each, all on the chip together or
+  // in rounds.
+  double rounds(int64_t groups, double slices, int cus) const {
     const double load = double(groups) / cus - (full - 1);
     const double at = load < 0.0 ? 0.0 : load > 1.0 ? 1.0 : load;
-    const double each = start + (slice + (slice_full - slice) * at) * double((slices + parts - 1) / parts);
-    const double join = parts > 1 ? 1.0 + 0.4 * parts + 8.0 * double(groups) * bm * bn / 5e6 : 0.0;
-    return double((groups + cus - 1) / cus) * each + join;
+    return double((groups + cus - 1) / cus) * (start + (slice + (slice_full - slice) * at) * slices);
+  }
+  double us(const Shares& s, int64_t tiles, int64_t slices, int cus) const {
+    const int64_t groups = (tiles - s.whole) * s.parts;
+    double t = rounds(groups, double((slices + s.parts - 1) / s.parts), cus);
+    if (s.whole) t += rounds(s.whole, double(slices), cus);
+    return s.parts > 1 ? t + 1.0 + 0.4 * s.parts + 8.0 * double(groups) * bm * bn / 5e6 : t;
   }
 };
 
 struct Choice {
-  int tile = 0, parts = 1;
+  int tile;
+  Shares shares;
+  unsigned groups;
 };
 
-// The tile shape and the parts of the long axis that cost least.
+// The tile shape and the shares that cost least: no tile, every tile, or the
+// tiles of the last, unfilled round in parts.
 template <int N>
-Choice choose(const TileCost (&tiles)[N], int64_t rows, int64_t cols, int64_t slices, const SplitSpace& split,
-              int cus) {
-  Choice best;
+Choice choose(const TileCost (&tiles)[N], int64_t rows, int64_t cols, int64_t slices, int64_t most_parts,
+              const SplitSpace& split, int cus) {
+  Choice best{};
   double least = -1.0;
   for (int t = 0; t < N; ++t) {
-    const int64_t count = (rows + tiles[t].bm - 1) / tiles[t].bm * ((cols + tiles[t].bn - 1) / tiles[t].bn);
-    for (int parts = 1; parts <= kMaxParts && parts <= slices; ++parts) {
-      if (parts > 1 && (count > kSplitCounts || count * parts * tiles[t].bm * tiles[t].bn > split.sum_floats)) break;
-      const double us = tiles[t].us(rows, cols, slices, parts, cus);
-      if (least < 0.0 || us < least) {
-        least = us;
-        best = Choice{t, parts};
+    const int64_t bm = tiles[t].bm, bn = tiles[t].bn;
+    const int64_t count = (rows + bm - 1) / bm * ((cols + bn - 1) / bn);
+    for (int parts = 1; parts <= kMaxParts && parts <= most_parts; ++parts)
+      for (int tail = 0; tail < 2; ++tail) {
+        const int64_t whole = tail ? count / cus * cus : 0, cut = count - whole;
+        if (tail && (parts == 1 || whole == 0 || cut == 0)) continue;
+        if (parts > 1 && (cut > kSplitCounts || cut * parts * bm * bn > split.sum_floats)) continue;
+        const Shares s{int(whole), parts};
+        const double us = tiles[t].us(s, count, slices, cus);
+        if (least < 0.0 || us < least) {
+          least = us;
+          best = Choice{t, s, unsigned(whole + cut * parts)};
+        }
       }
-    }
   }
   return best;
 }
@@ -852,22 +884,19 @@ hipError_t launch_product(DType out_t, Fp8 a_fmt, const BlocksRef& a, const Bloc
       return;
     }
     const int64_t blocks = (a.cols + kBlockCols - 1) / kBlockCols;
-    auto go = [&](auto k, const TileCost& t, int threads, int parts) {
-      const int64_t tiles = (c.rows + t.bm - 1) / t.bm * ((c.cols + t.bn - 1) / t.bn);
-      k<<<unsigned(tiles * parts), threads, 0, s>>>(a, b, c, accumulate, parts, split);
+    auto go = [&](auto k, const Choice& p, int threads) {
+      k<<<p.groups, threads, 0, s>>>(a, b, c, accumulate, p.shares, split);
     };
     if (out_t == DType::BF16) {
-      const Choice p = choose(kProductTiles, c.rows, c.cols, 2 * blocks, split, cus);
-      const int parts = p.parts <= blocks ? p.parts : int(blocks);
-      if (p.tile == 0) return go(k_product<bf16, F, 4, 2, 2, 4>, kProductTiles[0], 512, parts);
-      if (p.tile == 1) return go(k_product<bf16, F, 2, 2, 2, 2>, kProductTiles[1], 256, parts);
-      if (p.tile == 2) return go(k_product<bf16, F, 1, 2, 2, 2>, kProductTiles[2], 256, parts);
-      return go(k_product<bf16, F, 2, 2, 2, 4>, kProductTiles[3], 512, parts);
+      const Choice p = choose(kProductTiles, c.rows, c.cols, 2 * blocks, blocks, split, cus);
+      if (p.tile == 0) return go(k_product<bf16, F, 4, 2, 2, 4>, p, 512);
+      if (p.tile == 1) return go(k_product<bf16, F, 2, 2, 2, 2>, p, 256);
+      if (p.tile == 2) return go(k_product<bf16, F, 1, 2, 2, 2>, p, 256);
+      return go(k_product<bf16, F, 2, 2, 2, 4>, p, 512);
     }
-    const Choice p = choose(kProductExactTiles, c.rows, c.cols, 2 * blocks, split, cus);
-    const int parts = p.parts <= blocks ? p.parts : int(blocks);
-    if (p.tile == 0) return go(k_product<float, F, 2, 2, 2, 2>, kProductExactTiles[0], 256, parts);
-    return go(k_product<float, F, 1, 2, 2, 2>, kProductExactTiles[1], 256, parts);
+    const Choice p = choose(kProductExactTiles, c.rows, c.cols, 2 * blocks, blocks, split, cus);
+    if (p.tile == 0) return go(k_product<float, F, 2, 2, 2, 2>, p, 256);
+    return go(k_product<float, F, 1, 2, 2, 2>, p, 256);
   });
   return hipGetLastError();
 }
@@ -877,14 +906,11 @@ constexpr TileCost kWeightGradTiles[] = {{256, 256, 8.0, 0.64, 0.82, 1}, {128, 1
 
 hipError_t launch_weight_grad(DType out_t, Fp8 x_fmt, const BlocksRef& x, const DenseRef& dy, const DenseRef& dw,
                               bool accumulate, const SplitSpace& split, int cus, hipStream_t s) {
-  const Choice p = choose(kWeightGradTiles, dw.rows, dw.cols, (x.rows + 31) / 32, split, cus);
+  const int64_t slices = (x.rows + 31) / 32;
+  const Choice p = choose(kWeightGradTiles, dw.rows, dw.cols, slices, slices > 0 ? slices : 1, split, cus);
   with_fp8(x_fmt, [&](auto fmt) {
     constexpr Fp8 F = decltype(fmt)::value;
-    auto go = [&](auto k, int threads) {
-      const TileCost& t = kWeightGradTiles[p.tile];
-      const int64_t tiles = (dw.rows + t.bm - 1) / t.bm * ((dw.cols + t.bn - 1) / t.bn);
-      k<<<unsigned(tiles * p.parts), threads, 0, s>>>(x, dy, dw, accumulate, p.parts, split);
-    };
+    auto go = [&](auto k, int threads) { k<<<p.groups, threads, 0, s>>>(x, dy, dw, accumulate, p.shares, split); };
     if (out_t == DType::BF16)
       p.tile == 0 ? go(k_weight_grad<bf16, F, 4, 2, 2, 4>, 512) : go(k_weight_grad<bf16, F, 2, 2, 2, 2>, 256);
     else
