@@ -57,6 +57,14 @@ __device__ __forceinline__ void hold(V& v) {
 // for the copies that the pipeline keeps in flight.
 __device__ __forceinline__ void barrier_no_fence() { asm volatile("s_barrier" ::: "memory"); }
 
+// The wave's issue priority, 1 where `high`: in one block of assembly, because a
+// branch in a K loop would let the compiler move MFMAs across it.
+__device__ __forceinline__ void set_priority(int high) {
+  asm volatile(
+      "s_cmp_lg_u32 %0, 0\n\ts_cbranch_scc1 1f\n\ts_setprio 0\n\ts_branch 2f\n1:\n\ts_setprio 1\n2:" ::"s"(high)
+      : "scc");
+}
+
 __device__ __forceinline__ uint32_t lds_addr(const void* p) {
   return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((const lds_void_t*)p));
 }
@@ -337,6 +345,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_product(BlocksRef a, BlocksRef
 
   auto slice = [&](auto set, int kt) {
     constexpr int P = decltype(set)::value;
+    if constexpr (W == 8) set_priority((P + (wave >> 2)) & 1);
     const int shift = 8 * (kt >> 1 & 3);
     uint32_t sb[NF];
 #pragma unroll
