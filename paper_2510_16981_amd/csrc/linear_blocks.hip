@@ -2,9 +2,11 @@
 // activation with 8-bit checkpoints.  All stream their operands once and are
 // bound by memory.
 //
-// One wave holds one or more rows of one group of 512 columns: lane l has
-// columns 8 l .. 8 l + 7 (16 bytes of bf16 in, 8 bytes out), 16 lanes one block
-// of 128, and the wave one word of scales a row.
+// One wave holds one row of one group of 512 columns: lane l has columns 8 l ..
+// 8 l + 7 (16 bytes of bf16 in, 8 bytes out), 16 lanes one block of 128, and the
+// wave one word of scales.  (Two or four rows a wave were no faster on any size:
+// 16384 x 4096 quantized in 35.4 against 34.7 us, 64 x 4096 in 3.6 against 2.5;
+// gated forward 107 against 102 and 4.7 against 3.5.)
 #include "linear_device.h"
 
 namespace muonbp {
@@ -14,30 +16,23 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
 
-// The rows and the group of columns of this wave.
-template <int ROWS>
+// The row and the group of columns of this wave; neighbouring waves hold
+// neighbouring groups of a row.
 struct Strip {
-  int64_t r0;
-  int64_t group;
+  int64_t row, group, col;
   int lane;
-  int64_t col;
-  bool any;
-  __device__ __forceinline__ Strip(int64_t rows, int64_t cols) {
+  __device__ __forceinline__ explicit Strip(int64_t cols) {
     lane = threadIdx.x & 63;
-    const int64_t groups = (cols + kGroupCols - 1) / kGroupCols;
-    const int64_t w = int64_t(blockIdx.x) * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    // Neighbouring waves hold neighbouring groups of the same rows.
-    r0 = w / groups * ROWS;
+    const uint32_t groups = uint32_t((cols + kGroupCols - 1) / kGroupCols);
+    const uint32_t w = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    row = w / groups;
     group = w % groups;
     col = group * kGroupCols + 8 * lane;
-    any = r0 < rows;
   }
 };
 
-template <int ROWS>
 unsigned strip_blocks(int64_t rows, int64_t cols) {
-  const int64_t waves = (rows + ROWS - 1) / ROWS * ((cols + kGroupCols - 1) / kGroupCols);
-  return unsigned((waves + kWaves - 1) / kWaves);
+  return unsigned((rows * ((cols + kGroupCols - 1) / kGroupCols) + kWaves - 1) / kWaves);
 }
 
 // Eight values of a row (n of them inside the matrix) to 8 bits: the values
@@ -69,58 +64,42 @@ __device__ __forceinline__ int left(int64_t cols, int64_t col) {
 __device__ __forceinline__ bool block_in(int64_t cols, int64_t col) { return (col & ~int64_t(kBlockCols - 1)) < cols; }
 
 template <Fp8 F>
-__device__ __forceinline__ void store_blocks(const BlocksRef& o, int64_t row, int64_t group, int64_t col,
-                                             const float f[8], int lane) {
+__device__ __forceinline__ void store_blocks(const BlocksRef& o, const Strip& s, const float f[8]) {
   uint32_t byte;
   const u32x2_t q = round_block<F>(f, byte);
-  const bool in = block_in(o.cols, col);
-  if (in) gstore<u32x2_t, 8>(o.data + row * o.ld + col, q);
+  const bool in = block_in(o.cols, s.col);
+  if (in) gstore<u32x2_t, 8>(o.data + s.row * o.ld + s.col, q);
   const uint32_t w = scale_word(byte, in);
-  if (lane == 0) gstore<uint32_t, 4>(o.scales + group * o.scale_ld + row, w);
+  if (s.lane == 0) gstore<uint32_t, 4>(o.scales + s.group * o.scale_ld + s.row, w);
 }
 
 template <Fp8 F>
-__device__ __forceinline__ void load_blocks(const BlocksRef& x, int64_t row, int64_t group, int64_t col, int lane,
-                                            float f[8]) {
-  if (block_in(x.cols, col)) {
-    const uint32_t w = gload<uint32_t, 4>(x.scales + group * x.scale_ld + row);
-    unpack8<F>(gload<u32x2_t, 8>(x.data + row * x.ld + col), scale_of(w >> (8 * (lane >> 4)) & 255u), f);
+__device__ __forceinline__ void load_blocks(const BlocksRef& x, const Strip& s, float f[8]) {
+  if (block_in(x.cols, s.col)) {
+    const uint32_t w = gload<uint32_t, 4>(x.scales + s.group * x.scale_ld + s.row);
+    unpack8<F>(gload<u32x2_t, 8>(x.data + s.row * x.ld + s.col), scale_of(w >> (8 * (s.lane >> 4)) & 255u), f);
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i) f[i] = 0.f;
   }
 }
 
-constexpr int kQuantizeRows = 4;
-
 template <typename T, Fp8 F>
 __global__ __launch_bounds__(kThreads) void k_quantize(DenseRef x, BlocksRef out) {
-  const Strip<kQuantizeRows> s(x.rows, x.cols);
-  if (!s.any) return;
-  const int n = left(x.cols, s.col);
-  float f[kQuantizeRows][8];
-#pragma unroll
-  for (int r = 0; r < kQuantizeRows; ++r)
-    load8(static_cast<const T*>(x.ptr) + (s.r0 + r) * x.ld + s.col, s.r0 + r < x.rows ? n : 0, f[r]);
-#pragma unroll
-  for (int r = 0; r < kQuantizeRows; ++r)
-    if (s.r0 + r < x.rows) store_blocks<F>(out, s.r0 + r, s.group, s.col, f[r], s.lane);
+  const Strip s(x.cols);
+  if (s.row >= x.rows) return;
+  float f[8];
+  load8(static_cast<const T*>(x.ptr) + s.row * x.ld + s.col, left(x.cols, s.col), f);
+  store_blocks<F>(out, s, f);
 }
-
-constexpr int kRestoreRows = 4;
 
 template <typename T, Fp8 F>
 __global__ __launch_bounds__(kThreads) void k_restore(BlocksRef x, DenseRef out) {
-  const Strip<kRestoreRows> s(x.rows, x.cols);
-  if (!s.any) return;
-  const int n = left(x.cols, s.col);
-  float f[kRestoreRows][8];
-#pragma unroll
-  for (int r = 0; r < kRestoreRows; ++r)
-    if (s.r0 + r < x.rows) load_blocks<F>(x, s.r0 + r, s.group, s.col, s.lane, f[r]);
-#pragma unroll
-  for (int r = 0; r < kRestoreRows; ++r)
-    if (s.r0 + r < x.rows) store8(static_cast<T*>(out.ptr) + (s.r0 + r) * out.ld + s.col, n, f[r]);
+  const Strip s(x.cols);
+  if (s.row >= x.rows) return;
+  float f[8];
+  load_blocks<F>(x, s, f);
+  store8(static_cast<T*>(out.ptr) + s.row * out.ld + s.col, left(x.cols, s.col), f);
 }
 
 // One workgroup a 128 x 128 tile: thread t has columns 8 (t % 16) .. + 7 of rows
@@ -205,78 +184,54 @@ __device__ __forceinline__ void logistic(float g, float& s, float& rest) {
   rest = g >= 0.f ? q : r;
 }
 
-constexpr int kGatedRows = 2;
-
 template <typename T, Fp8 FK, Fp8 FH>
 __global__ __launch_bounds__(kThreads) void k_gated_forward(DenseRef gate, DenseRef up, DenseRef h, BlocksRef h8,
                                                             BlocksRef gate8, BlocksRef up8) {
-  const Strip<kGatedRows> s(gate.rows, gate.cols);
-  if (!s.any) return;
+  const Strip s(gate.cols);
+  if (s.row >= gate.rows) return;
   const int n = left(gate.cols, s.col);
-  float g[kGatedRows][8], u[kGatedRows][8];
-#pragma unroll
-  for (int r = 0; r < kGatedRows; ++r) {
-    const int m = s.r0 + r < gate.rows ? n : 0;
-    load8(static_cast<const T*>(gate.ptr) + (s.r0 + r) * gate.ld + s.col, m, g[r]);
-    load8(static_cast<const T*>(up.ptr) + (s.r0 + r) * up.ld + s.col, m, u[r]);
+  float g[8], u[8], y[8];
+  load8(static_cast<const T*>(gate.ptr) + s.row * gate.ld + s.col, n, g);
+  load8(static_cast<const T*>(up.ptr) + s.row * up.ld + s.col, n, u);
+  if (gate8.data) {
+    store_blocks<FK>(gate8, s, g);
+    store_blocks<FK>(up8, s, u);
   }
 #pragma unroll
-  for (int r = 0; r < kGatedRows; ++r) {
-    const int64_t row = s.r0 + r;
-    if (row >= gate.rows) break;
-    if (gate8.data) {
-      store_blocks<FK>(gate8, row, s.group, s.col, g[r], s.lane);
-      store_blocks<FK>(up8, row, s.group, s.col, u[r], s.lane);
-    }
-    float y[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      float l, rest;
-      logistic(g[r][i], l, rest);
-      y[i] = g[r][i] * l * u[r][i];
-    }
-    if (h.ptr) store8(static_cast<T*>(h.ptr) + row * h.ld + s.col, n, y);
-    if (h8.data) store_blocks<FH>(h8, row, s.group, s.col, y, s.lane);
+  for (int i = 0; i < 8; ++i) {
+    float l, rest;
+    logistic(g[i], l, rest);
+    y[i] = g[i] * l * u[i];
   }
+  if (h.ptr) store8(static_cast<T*>(h.ptr) + s.row * h.ld + s.col, n, y);
+  if (h8.data) store_blocks<FH>(h8, s, y);
 }
 
 template <typename T, Fp8 FK, Fp8 FD>
 __global__ __launch_bounds__(kThreads) void k_gated_backward(DenseRef dh, BlocksRef gate, BlocksRef up,
                                                              DenseRef dgate, DenseRef dup, BlocksRef dgate8,
                                                              BlocksRef dup8) {
-  const Strip<kGatedRows> s(dh.rows, dh.cols);
-  if (!s.any) return;
+  const Strip s(dh.cols);
+  if (s.row >= dh.rows) return;
   const int n = left(dh.cols, s.col);
-  float d[kGatedRows][8], g[kGatedRows][8], u[kGatedRows][8];
+  float d[8], g[8], u[8], dg[8], du[8];
+  load8(static_cast<const T*>(dh.ptr) + s.row * dh.ld + s.col, n, d);
+  load_blocks<FK>(gate, s, g);
+  load_blocks<FK>(up, s, u);
 #pragma unroll
-  for (int r = 0; r < kGatedRows; ++r) {
-    const int64_t row = s.r0 + r;
-    load8(static_cast<const T*>(dh.ptr) + row * dh.ld + s.col, row < dh.rows ? n : 0, d[r]);
-    if (row < dh.rows) {
-      load_blocks<FK>(gate, row, s.group, s.col, s.lane, g[r]);
-      load_blocks<FK>(up, row, s.group, s.col, s.lane, u[r]);
-    }
+  for (int i = 0; i < 8; ++i) {
+    float l, rest;
+    logistic(g[i], l, rest);
+    du[i] = d[i] * (g[i] * l);
+    dg[i] = d[i] * u[i] * (l * (1.f + g[i] * rest));
   }
-#pragma unroll
-  for (int r = 0; r < kGatedRows; ++r) {
-    const int64_t row = s.r0 + r;
-    if (row >= dh.rows) break;
-    float dg[8], du[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      float l, rest;
-      logistic(g[r][i], l, rest);
-      du[i] = d[r][i] * (g[r][i] * l);
-      dg[i] = d[r][i] * u[r][i] * (l * (1.f + g[r][i] * rest));
-    }
-    if (dgate.ptr) {
-      store8(static_cast<T*>(dgate.ptr) + row * dgate.ld + s.col, n, dg);
-      store8(static_cast<T*>(dup.ptr) + row * dup.ld + s.col, n, du);
-    }
-    if (dgate8.data) {
-      store_blocks<FD>(dgate8, row, s.group, s.col, dg, s.lane);
-      store_blocks<FD>(dup8, row, s.group, s.col, du, s.lane);
-    }
+  if (dgate.ptr) {
+    store8(static_cast<T*>(dgate.ptr) + s.row * dgate.ld + s.col, n, dg);
+    store8(static_cast<T*>(dup.ptr) + s.row * dup.ld + s.col, n, du);
+  }
+  if (dgate8.data) {
+    store_blocks<FD>(dgate8, s, dg);
+    store_blocks<FD>(dup8, s, du);
   }
 }
 
@@ -301,8 +256,7 @@ void with_format(Fp8 v, F&& f) {
 hipError_t launch_quantize(DType in_t, Fp8 fmt, const DenseRef& x, const BlocksRef& out, hipStream_t s) {
   with_type(in_t, [&](auto t) {
     with_format(fmt, [&](auto f) {
-      k_quantize<decltype(t), decltype(f)::value>
-          <<<strip_blocks<kQuantizeRows>(x.rows, x.cols), kThreads, 0, s>>>(x, out);
+      k_quantize<decltype(t), decltype(f)::value><<<strip_blocks(x.rows, x.cols), kThreads, 0, s>>>(x, out);
     });
   });
   return hipGetLastError();
@@ -323,8 +277,7 @@ hipError_t launch_quantize_weight(DType in_t, Fp8 fmt, const DenseRef& w, const 
 hipError_t launch_restore(DType out_t, Fp8 fmt, const BlocksRef& x, const DenseRef& out, hipStream_t s) {
   with_type(out_t, [&](auto t) {
     with_format(fmt, [&](auto f) {
-      k_restore<decltype(t), decltype(f)::value>
-          <<<strip_blocks<kRestoreRows>(x.rows, x.cols), kThreads, 0, s>>>(x, out);
+      k_restore<decltype(t), decltype(f)::value><<<strip_blocks(x.rows, x.cols), kThreads, 0, s>>>(x, out);
     });
   });
   return hipGetLastError();
@@ -337,7 +290,7 @@ hipError_t launch_gated_forward(DType t, const DenseRef& gate, const DenseRef& u
     with_format(kept_fmt, [&](auto fk) {
       with_format(h_fmt, [&](auto fh) {
         k_gated_forward<decltype(e), decltype(fk)::value, decltype(fh)::value>
-            <<<strip_blocks<kGatedRows>(gate.rows, gate.cols), kThreads, 0, s>>>(gate, up, h, h8, gate8, up8);
+            <<<strip_blocks(gate.rows, gate.cols), kThreads, 0, s>>>(gate, up, h, h8, gate8, up8);
       });
     });
   });
@@ -351,7 +304,7 @@ hipError_t launch_gated_backward(DType t, const DenseRef& dh, const BlocksRef& g
     with_format(kept_fmt, [&](auto fk) {
       with_format(d_fmt, [&](auto fd) {
         k_gated_backward<decltype(e), decltype(fk)::value, decltype(fd)::value>
-            <<<strip_blocks<kGatedRows>(dh.rows, dh.cols), kThreads, 0, s>>>(dh, gate, up, dgate, dup, dgate8, dup8);
+            <<<strip_blocks(dh.rows, dh.cols), kThreads, 0, s>>>(dh, gate, up, dgate, dup, dgate8, dup8);
       });
     });
   });

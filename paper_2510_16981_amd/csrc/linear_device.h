@@ -39,7 +39,8 @@ __device__ __forceinline__ uint32_t f_bits(float f) { return __builtin_bit_cast(
 __device__ __forceinline__ float to_f(float x) { return x; }
 __device__ __forceinline__ float to_f(bf16 x) { return float(x); }
 
-// f <- n <= 8 consecutive elements at p, zeros past them.
+// f <- n <= 8 consecutive elements at p, zeros past them.  (One by one, all are
+// loaded before the first is used: past n, the first element again.)
 __device__ __forceinline__ void load8(const bf16* p, int n, float f[8]) {
   if (n >= 8) {
     const u32x4_t v = gload<u32x4_t, 2>(p);
@@ -48,9 +49,15 @@ __device__ __forceinline__ void load8(const bf16* p, int n, float f[8]) {
       f[2 * i] = bits_f(v[i] << 16);
       f[2 * i + 1] = bits_f(v[i] & 0xffff0000u);
     }
+  } else if (n > 0) {
+    uint32_t h[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) h[i] = gload<uint16_t, 2>(p + (i < n ? i : 0));
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = i < n ? bits_f(h[i] << 16) : 0.f;
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = i < n ? bits_f(uint32_t(gload<uint16_t, 2>(p + i)) << 16) : 0.f;
+    for (int i = 0; i < 8; ++i) f[i] = 0.f;
   }
 }
 __device__ __forceinline__ void load8(const float* p, int n, float f[8]) {
@@ -61,9 +68,15 @@ __device__ __forceinline__ void load8(const float* p, int n, float f[8]) {
       f[i] = a[i];
       f[i + 4] = b[i];
     }
+  } else if (n > 0) {
+    float h[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) h[i] = gload<float, 4>(p + (i < n ? i : 0));
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = i < n ? h[i] : 0.f;
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = i < n ? gload<float, 4>(p + i) : 0.f;
+    for (int i = 0; i < 8; ++i) f[i] = 0.f;
   }
 }
 

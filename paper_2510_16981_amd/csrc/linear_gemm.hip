@@ -261,7 +261,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_product(BlocksRef a, BlocksRef
 
   // Slices of this part: whole blocks of 128.
   const int nblk = int(kbytes / kBlockCols);
-  const int kb = 2 * int(int64_t(t.part) * nblk / t.parts), ke = 2 * int(int64_t(t.part + 1) * nblk / t.parts);
+  const int kb = 2 * (t.part * nblk / t.parts), ke = 2 * ((t.part + 1) * nblk / t.parts);
 
   uint32_t voff[LP];
 #pragma unroll
@@ -589,9 +589,8 @@ __global__ __launch_bounds__(64 * WM * WN) void k_weight_grad(BlocksRef x, Dense
   const int wm = wave / WN, wn = wave % WN;
   // Slices of this part, in the order ke - 1, ke - 2, kb, kb + 1, ...
   const int64_t tokens = x.rows;
-  const int64_t nk = (tokens + KT - 1) / KT;
-  const int64_t kb = t.part * nk / t.parts, ke = (t.part + 1) * nk / t.parts;
-  const int count = int(ke - kb);
+  const int nk = int((tokens + KT - 1) / KT);  // at most 2^21, times 8 parts
+  const int kb = t.part * nk / t.parts, ke = (t.part + 1) * nk / t.parts, count = ke - kb;
 
   const int64_t padded = (x.cols + kBlockCols - 1) / kBlockCols * kBlockCols;
   uint32_t xoff[XC], xlds[XC], yoff[YC], ylds[YC];
