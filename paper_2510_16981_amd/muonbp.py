@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import List, Optional, Sequence, Tuple
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -91,6 +92,7 @@ class Profile(ctypes.Structure):
 
 
 _lib = None
+_torch = None  # set with _lib
 
 
 def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
@@ -100,13 +102,14 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     same soname as the system one, and the library must bind to the runtime
     that owns torch's memory and streams (loaded the other way round, the
     process would end up with two runtimes)."""
-    global _lib
+    global _lib, _torch
     if _lib is not None:
         return _lib
     if not os.path.exists(path):
         raise RuntimeError(
             f"{path} is missing: build it with `python -m paper_2510_16981_amd.build`")
-    import torch  # noqa: F401  (see above)
+    import torch
+    _torch = torch
     lib = ctypes.CDLL(path)
     P, I32, I64, F = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float
     sig = {
@@ -475,34 +478,39 @@ class AdamW:
 BLOCK_COLS, GROUP_COLS = 128, 512
 
 
+# muonbp_dense and muonbp_blocks as bytes, which take a third of the time of a
+# ctypes.Structure to make and are passed by address as they are.
+_DENSE = struct.Struct("Pqqqi4x")
+_BLOCKS = struct.Struct("PPqqqqi4x")
+
+
 class Blocks:
     """A matrix in 8-bit floating point with a power-of-two scale for each
     block of 128 columns of a row (muonbp_blocks): ``data`` is uint8, rows x
     (cols rounded up to 128 at least), ``scales`` int32, ceil(cols / 512) x
     rows, a byte for each block.  Holds its tensors; makes no copy."""
 
-    __slots__ = ("_data", "_scales", "_memory", "rows", "cols", "format", "device", "ref", "addr")
+    __slots__ = ("_data", "_scales", "_memory", "rows", "cols", "ld", "format", "device", "ref")
 
     def __init__(self, data, scales, cols: int, format: int = E4M3):
-        import torch
+        if _torch is None:
+            load_library()
         rows, width = data.shape
         groups = -(-cols // GROUP_COLS)
-        if not (data.dtype is torch.uint8 and data.is_cuda and data.stride(1) == 1
+        if not (data.dtype is _torch.uint8 and data.is_cuda and data.stride(1) == 1
                 and width >= -(-cols // BLOCK_COLS) * BLOCK_COLS):
             raise ValueError(f"data: need a CUDA uint8 matrix with rows of at least {cols} bytes rounded up "
                              f"to {BLOCK_COLS}, got {data.dtype} {tuple(data.shape)}")
-        if not (scales.shape == (groups, rows) and scales.dtype is torch.int32
-                and scales.device == data.device and (rows <= 1 or scales.stride(1) == 1)):
-            raise ValueError(f"scales: need an int32 matrix of shape {(groups, rows)} on {data.device}, "
+        device = data.device
+        if not (scales.shape == (groups, rows) and scales.dtype is _torch.int32
+                and scales.device == device and (rows <= 1 or scales.stride(1) == 1)):
+            raise ValueError(f"scales: need an int32 matrix of shape {(groups, rows)} on {device}, "
                              f"got {scales.dtype} {tuple(scales.shape)}")
         self._data, self._scales, self._memory = data, scales, None
-        self._describe(data.data_ptr(), scales.data_ptr(), rows, cols, data.stride(0) if rows > 1 else width,
-                       scales.stride(0) if groups > 1 else rows, format, data.device)
-
-    def _describe(self, data, scales, rows, cols, ld, scale_ld, format, device):
         self.rows, self.cols, self.format, self.device = rows, cols, format, device
-        self.ref = BlocksRef(data, scales, rows, cols, ld, scale_ld, format)
-        self.addr = ctypes.addressof(self.ref)
+        self.ld = data.stride(0) if rows > 1 else width
+        self.ref = _BLOCKS.pack(data.data_ptr(), scales.data_ptr(), rows, cols, self.ld,
+                                scales.stride(0) if groups > 1 else rows, format)
 
     @classmethod
     def _in(cls, memory, rows: int, cols: int, ld: int, format: int) -> "Blocks":
@@ -510,23 +518,22 @@ class Blocks:
         self = object.__new__(cls)
         self._data = self._scales = None
         self._memory = memory
+        self.rows, self.cols, self.ld, self.format, self.device = rows, cols, ld, format, memory.device
         at = memory.data_ptr()
-        self._describe(at, at + rows * ld, rows, cols, ld, rows, format, memory.device)
+        self.ref = _BLOCKS.pack(at, at + rows * ld, rows, cols, ld, rows, format)
         return self
 
     @property
     def data(self):
         if self._data is None:
-            rows, ld = self.rows, self.ref.ld
-            self._data = self._memory[:rows * ld].view(rows, ld)
+            self._data = self._memory[:self.rows * self.ld].view(self.rows, self.ld)
         return self._data
 
     @property
     def scales(self):
         if self._scales is None:
-            import torch
-            rows, ld = self.rows, self.ref.ld
-            self._scales = self._memory[rows * ld:].view(torch.int32).view(-(-self.cols // GROUP_COLS), rows)
+            self._scales = self._memory[self.rows * self.ld:].view(_torch.int32).view(
+                -(-self.cols // GROUP_COLS), self.rows)
         return self._scales
 
     def __getitem__(self, rows: slice) -> "Blocks":
@@ -561,7 +568,6 @@ class Linear:
         self.ctx = ctx
         self._stream = stream
         self.device = stream.device
-        self._torch = torch
         self._codes = {torch.float32: F32, torch.bfloat16: BF16}
         # The handle of the current stream: torch.cuda.current_stream builds an
         # object for it, which takes longer than the rest of a call.
@@ -574,7 +580,7 @@ class Linear:
             detail = self.lib.muonbp_linear_last_error(self.ctx)
             raise MuonBPError(st, f"{what}: {detail.decode() if detail else ''}")
 
-    def _dense(self, t, name: str) -> Dense:
+    def _dense(self, t, name: str) -> bytes:
         code = self._codes.get(t.dtype)
         if code is None or t.dim() != 2 or t.device != self.device:
             raise ValueError(f"{name}: need a bf16 or fp32 matrix on {self.device}, got {t.dtype} "
@@ -583,15 +589,23 @@ class Linear:
         ld, inner = t.stride()
         if (inner != 1 and cols > 1) or (ld < cols and rows > 1):
             raise ValueError(f"{name}: need contiguous rows, got strides {t.stride()}")
-        return Dense(t.data_ptr(), rows, cols, ld if rows > 1 else cols, code)
+        return _DENSE.pack(t.data_ptr(), rows, cols, ld if rows > 1 else cols, code)
 
-    def _blocks(self, b: Blocks, name: str):
+    def _new(self, rows: int, cols: int, dtype):
+        """(A new matrix, its muonbp_dense.)"""
+        t = self._empty((rows, cols), dtype)
+        code = self._codes.get(dtype)
+        if code is None:
+            raise ValueError(f"need bf16 or fp32, got {dtype}")
+        return t, _DENSE.pack(t.data_ptr(), rows, cols, cols, code)
+
+    def _blocks(self, b: Blocks, name: str) -> bytes:
         if not isinstance(b, Blocks) or b.device != self.device:
             raise ValueError(f"{name}: need Blocks on {self.device}")
-        return b.addr
+        return b.ref
 
     def _empty(self, shape, dtype):
-        torch = self._torch
+        torch = _torch
         if self._current(self.device.index) == self._stream.cuda_stream:
             return torch.empty(shape, dtype=dtype, device=self.device)
         with torch.cuda.stream(self._stream):
@@ -600,7 +614,7 @@ class Linear:
     def empty_blocks(self, rows: int, cols: int, format: int = E4M3) -> Blocks:
         """Uninitialised Blocks of rows x cols."""
         ld = -(-cols // BLOCK_COLS) * BLOCK_COLS
-        return Blocks._in(self._empty(rows * (ld + 4 * -(-cols // GROUP_COLS)), self._torch.uint8), rows, cols, ld,
+        return Blocks._in(self._empty(rows * (ld + 4 * -(-cols // GROUP_COLS)), _torch.uint8), rows, cols, ld,
                           format)
 
     # -- API
@@ -608,80 +622,87 @@ class Linear:
         """x in 8 bits, one scale for each block of 128 columns of a row."""
         d = self._dense(x, "x")
         if out is None:
-            out = self.empty_blocks(d.rows, d.cols, format)
-        self._check(self.lib.muonbp_linear_quantize(self.ctx, ctypes.addressof(d), self._blocks(out, "out")),
-                    "quantize")
+            out = self.empty_blocks(x.shape[0], x.shape[1], format)
+        self._check(self.lib.muonbp_linear_quantize(self.ctx, d, self._blocks(out, "out")), "quantize")
         return out
 
     def quantize_weight(self, w, format: int = E4M3, out: Optional[Blocks] = None,
                         out_t: Optional[Blocks] = None) -> Tuple[Blocks, Blocks]:
         """(w, its transpose) in 8 bits, one scale for each 128 x 128 tile."""
         d = self._dense(w, "w")
+        rows, cols = w.shape
         if out is None:
-            out = self.empty_blocks(d.rows, d.cols, format)
+            out = self.empty_blocks(rows, cols, format)
         if out_t is None:
-            out_t = self.empty_blocks(d.cols, d.rows, format)
-        self._check(self.lib.muonbp_linear_quantize_weight(self.ctx, ctypes.addressof(d),
-                                                           self._blocks(out, "out"),
+            out_t = self.empty_blocks(cols, rows, format)
+        self._check(self.lib.muonbp_linear_quantize_weight(self.ctx, d, self._blocks(out, "out"),
                                                            self._blocks(out_t, "out_t")), "quantize_weight")
         return out, out_t
 
     def restore(self, x: Blocks, dtype=None, out=None):
         """The values of x (bf16 by default), exact."""
-        a = self._blocks(x, "x")
+        px = self._blocks(x, "x")
         if out is None:
-            out = self._empty((x.rows, x.cols), dtype or self._torch.bfloat16)
-        d = self._dense(out, "out")
-        self._check(self.lib.muonbp_linear_restore(self.ctx, a, ctypes.addressof(d)), "restore")
+            out, d = self._new(x.rows, x.cols, dtype or _torch.bfloat16)
+        else:
+            d = self._dense(out, "out")
+        self._check(self.lib.muonbp_linear_restore(self.ctx, px, d), "restore")
+        return out
+
+    def _product(self, call, what, pa, pb, rows, cols, dtype, out, accumulate):
+        if out is None:
+            if accumulate:
+                raise ValueError("accumulate needs out")
+            out, d = self._new(rows, cols, dtype or _torch.bfloat16)
+        else:
+            d = self._dense(out, "out")
+        self._check(call(self.ctx, pa, pb, d, accumulate), what)
         return out
 
     def product(self, a: Blocks, b: Blocks, dtype=None, out=None, accumulate: bool = False):
         """a b^T (bf16 by default); ``accumulate`` adds it to ``out``."""
         pa, pb = self._blocks(a, "a"), self._blocks(b, "b")
-        if out is None:
-            if accumulate:
-                raise ValueError("accumulate needs out")
-            out = self._empty((a.rows, b.rows), dtype or self._torch.bfloat16)
-        d = self._dense(out, "out")
-        self._check(self.lib.muonbp_linear_product(self.ctx, pa, pb, ctypes.addressof(d), int(accumulate)),
-                    "product")
-        return out
+        return self._product(self.lib.muonbp_linear_product, "product", pa, pb, a.rows, b.rows, dtype, out,
+                             accumulate)
 
     def weight_grad(self, x: Blocks, dy, dtype=None, out=None, accumulate: bool = False):
         """x^T dy (bf16 by default); ``accumulate`` adds it to ``out``."""
-        px, dd = self._blocks(x, "x"), self._dense(dy, "dy")
-        if out is None:
-            if accumulate:
-                raise ValueError("accumulate needs out")
-            out = self._empty((x.cols, dd.cols), dtype or self._torch.bfloat16)
-        d = self._dense(out, "out")
-        self._check(self.lib.muonbp_linear_weight_grad(self.ctx, px, ctypes.addressof(dd), ctypes.addressof(d),
-                                                       int(accumulate)), "weight_grad")
-        return out
+        px, pd = self._blocks(x, "x"), self._dense(dy, "dy")
+        return self._product(self.lib.muonbp_linear_weight_grad, "weight_grad", px, pd, x.cols, dy.shape[1], dtype,
+                             out, accumulate)
 
     def gated_forward(self, gate, up, blocks: bool = False, keep: bool = True, format: int = E4M3):
         """(h, gate, up) with h = silu(gate) up of the inputs' dtype (``blocks``:
         in 8 bits) and gate and up kept in 8 bits (None without ``keep``)."""
         g, u = self._dense(gate, "gate"), self._dense(up, "up")
-        h = self.empty_blocks(g.rows, g.cols, format) if blocks else self._empty((g.rows, g.cols), gate.dtype)
-        dense = None if blocks else self._dense(h, "h")
-        g8, u8 = (self.empty_blocks(g.rows, g.cols, format) if keep else None for _ in range(2))
-        self._check(self.lib.muonbp_linear_gated_forward(
-            self.ctx, ctypes.addressof(g), ctypes.addressof(u), None if blocks else ctypes.addressof(dense),
-            h.addr if blocks else None, g8.addr if keep else None, u8.addr if keep else None), "gated_forward")
-        return h, g8, u8
+        rows, cols = gate.shape
+        d = h8 = g8 = u8 = None
+        if blocks:
+            h = self.empty_blocks(rows, cols, format)
+            h8 = h.ref
+        else:
+            h, d = self._new(rows, cols, gate.dtype)
+        kept = (None, None)
+        if keep:
+            kept = self.empty_blocks(rows, cols, format), self.empty_blocks(rows, cols, format)
+            g8, u8 = kept[0].ref, kept[1].ref
+        self._check(self.lib.muonbp_linear_gated_forward(self.ctx, g, u, d, h8, g8, u8), "gated_forward")
+        return h, kept[0], kept[1]
 
     def gated_backward(self, dh, gate: Blocks, up: Blocks, blocks: bool = False, format: int = E4M3):
         """(dgate, dup) of dh's dtype, and with ``blocks`` both in 8 bits too."""
         d = self._dense(dh, "dh")
         pg, pu = self._blocks(gate, "gate"), self._blocks(up, "up")
-        dgate, dup = (self._empty((d.rows, d.cols), dh.dtype) for _ in range(2))
-        a, b = self._dense(dgate, "dgate"), self._dense(dup, "dup")
-        dgate8, dup8 = (self.empty_blocks(d.rows, d.cols, format) if blocks else None for _ in range(2))
-        self._check(self.lib.muonbp_linear_gated_backward(
-            self.ctx, ctypes.addressof(d), pg, pu, ctypes.addressof(a), ctypes.addressof(b),
-            dgate8.addr if blocks else None, dup8.addr if blocks else None), "gated_backward")
-        return (dgate, dup, dgate8, dup8) if blocks else (dgate, dup)
+        rows, cols = dh.shape
+        (dgate, a), (dup, b) = self._new(rows, cols, dh.dtype), self._new(rows, cols, dh.dtype)
+        if not blocks:
+            self._check(self.lib.muonbp_linear_gated_backward(self.ctx, d, pg, pu, a, b, None, None),
+                        "gated_backward")
+            return dgate, dup
+        dgate8, dup8 = self.empty_blocks(rows, cols, format), self.empty_blocks(rows, cols, format)
+        self._check(self.lib.muonbp_linear_gated_backward(self.ctx, d, pg, pu, a, b, dgate8.ref, dup8.ref),
+                    "gated_backward")
+        return dgate, dup, dgate8, dup8
 
     def set_stream(self, stream) -> None:
         self._check(self.lib.muonbp_linear_set_stream(self.ctx, ctypes.c_void_p(stream.cuda_stream)),

@@ -519,18 +519,23 @@ def test_refusals(lin):
         return st
 
     lib, at = lin.lib, ctypes.addressof
-    d = lin._dense(x, "x")
+
+    def dense(t):
+        return mb.Dense.from_buffer_copy(lin._dense(t, "t"))
+
+    d = dense(x)
     o = lin.empty_blocks(8, 256)
-    assert status(lib.muonbp_linear_quantize, None, o.addr) == 1
+    assert status(lib.muonbp_linear_quantize, None, o.ref) == 1
     assert status(lib.muonbp_linear_quantize, at(d), None) == 1
     assert b"out" in lib.muonbp_linear_last_error(lin.ctx)
     for field, value, want in (("cols", 255, 2), ("rows", -1, 2), ("ld", 255, 2), ("dtype", 9, 3), ("ptr", None, 1),
                                ("ptr", d.ptr + 2, 1), ("cols", 0, 2), ("ld", 1 << 40, 2)):
-        e = lin._dense(x, "x")
+        e = dense(x)
         setattr(e, field, value)
-        assert status(lib.muonbp_linear_quantize, at(e), o.addr) == want, (field, value)
+        assert status(lib.muonbp_linear_quantize, at(e), o.ref) == want, (field, value)
     for field, value, want in (("ld", 250, 2), ("ld", 264, 2), ("scale_ld", 7, 2), ("format", 2, 1), ("data", None, 1),
-                               ("scales", None, 1), ("data", o.ref.data + 8, 1), ("scales", o.ref.scales + 2, 1),
+                               ("scales", None, 1), ("data", o.data.data_ptr() + 8, 1),
+                               ("scales", o.scales.data_ptr() + 2, 1),
                                ("cols", (1 << 22) + 1, 2), ("rows", 9, 2)):
         e = mb.BlocksRef.from_buffer_copy(o.ref)
         setattr(e, field, value)
@@ -539,20 +544,20 @@ def test_refusals(lin):
     over = mb.BlocksRef.from_buffer_copy(o.ref)
     over.data = d.ptr
     assert status(lib.muonbp_linear_quantize, at(d), at(over)) == 1
-    assert status(lib.muonbp_linear_gated_forward, at(d), at(d), None, o.addr, o.addr, b.addr) == 1
+    assert status(lib.muonbp_linear_gated_forward, at(d), at(d), None, o.ref, o.ref, b.ref) == 1
     y = torch.empty(8, 8, device="cuda")
-    c = lin._dense(y, "y")
+    c = dense(y)
     e5 = lin.quantize(x, mb.E5M2)
-    assert status(lib.muonbp_linear_product, b.addr, e5.addr, at(c), 0) == 1  # b in e5m2
-    assert status(lib.muonbp_linear_product, b.addr, b.addr, at(c), 2) == 1
-    assert status(lib.muonbp_linear_product, b.addr, lin.quantize(x[:, :100]).addr, at(c), 0) == 2
-    assert status(lib.muonbp_linear_product, b[:7].addr, b.addr, at(c), 0) == 2
-    assert status(lib.muonbp_linear_weight_grad, b.addr, at(d), at(c), 0) == 3  # dy in fp32
-    g = lin._dense(x, "x")
+    assert status(lib.muonbp_linear_product, b.ref, e5.ref, at(c), 0) == 1  # b in e5m2
+    assert status(lib.muonbp_linear_product, b.ref, b.ref, at(c), 2) == 1
+    assert status(lib.muonbp_linear_product, b.ref, lin.quantize(x[:, :100]).ref, at(c), 0) == 2
+    assert status(lib.muonbp_linear_product, b[:7].ref, b.ref, at(c), 0) == 2
+    assert status(lib.muonbp_linear_weight_grad, b.ref, at(d), at(c), 0) == 3  # dy in fp32
+    g = dense(x)
     assert status(lib.muonbp_linear_gated_forward, at(d), at(g), None, None, None, None) == 1
-    assert status(lib.muonbp_linear_gated_forward, at(d), at(g), None, o.addr, b.addr, None) == 1
-    assert status(lib.muonbp_linear_gated_backward, at(d), b.addr, b.addr, None, None, None, None) == 1
+    assert status(lib.muonbp_linear_gated_forward, at(d), at(g), None, o.ref, b.ref, None) == 1
+    assert status(lib.muonbp_linear_gated_backward, at(d), b.ref, b.ref, None, None, None, None) == 1
     assert status(lib.muonbp_linear_quantize_weight, at(d), None, None) == 1
-    assert status(lib.muonbp_linear_quantize_weight, at(d), None, o.addr) == 2
+    assert status(lib.muonbp_linear_quantize_weight, at(d), None, o.ref) == 2
     lin.quantize(x, out=o)  # still works
     assert torch.equal(o.data, b.data)
