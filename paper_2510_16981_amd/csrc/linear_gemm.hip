@@ -803,6 +803,208 @@ __global__ __launch_bounds__(64 * WM * WN) void k_weight_grad(BlocksRef x, Dense
                         o0 + wn * 32 * TN, accumulate);
 }
 
+// ---------------------------------------------------------------- weight gradient, few tiles
+//
+// Tiles of 64 x 64 whose four waves share the slices: each takes every fourth
+// one, of the whole tile, through 8 KB of LDS of its own.  One wave's LDS accesses
+// are done in order, so the loop has no barrier and no wait but for the operands;
+// the four sums then meet in LDS, each wave finishing one 32 x 32 quarter.  For
+// matrices of few tiles, where a 128 x 128 tile leaves most CUs idle and takes four
+// times the slices.  Measured against that tile, each in its best number of
+// parts, us: 333 tokens, 650 x 975 6.8 against 10.9; 512, 1024 x 1024 6.4 against
+// 9.9; 16384, 512 x 512 24 against 34; but 512, 2048 x 2048 15.5 against 11.0.
+//
+// Rows (tokens) of 64 elements, 128 bytes; 16-byte chunk c of row r at
+// c ^ 4 (r / 2 % 2): the 4 rows x 64 bytes of a transpose read are on all banks.
+template <typename T, Fp8 F>
+__global__ __launch_bounds__(256) void k_weight_grad_waves(BlocksRef x, DenseRef dy, DenseRef dw, bool accumulate,
+                                                           Shares shares, SplitSpace split) {
+  constexpr int B = 64, W = 4, KT = 32, PITCH = 2 * B, SLOT = 2 * KT * PITCH, XC = 2, YC = 4;
+  constexpr int SUMS = W * 3 * 32 * 32 * 4;  // three quarters of every wave
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[SUMS > W * SLOT ? SUMS : W * SLOT];
+  __shared__ int last;
+
+  const int tall = int((dw.rows + B - 1) / B), wide = int((dw.cols + B - 1) / B);
+  const TileAt t = tile_at(blockIdx.x, gridDim.x, tall, wide, shares);
+  const int64_t i0 = int64_t(t.ti) * B, o0 = int64_t(t.tj) * B;
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t tokens = x.rows;
+  const int nk = int((tokens + KT - 1) / KT);
+  const int kb = t.part * nk / t.parts, ke = (t.part + 1) * nk / t.parts;
+  // This wave's slices: ke - 1 - wave, then every fourth before it.
+  const int first = ke - 1 - wave, count = first >= kb ? (first - kb) / W + 1 : 0;
+
+  // Lane l has 32 features of token l / 2, and 8 columns of tokens l / 8 + 8 j.
+  const int64_t padded = (x.cols + kBlockCols - 1) / kBlockCols * kBlockCols;
+  const int xt = lane >> 1, xc = 32 * (lane & 1), yt = lane >> 3;
+  const int ycol = o0 + 8 * (lane & 7) < dy.cols ? 8 * (lane & 7) : 0;
+  const uint32_t xoff = uint32_t(xt) * uint32_t(x.ld) + (i0 + xc < padded ? xc : 0);
+  const uint32_t xshift = 8 * uint32_t(i0 / kBlockCols % 4);
+  const uint8_t* const xbase = x.data + i0;
+  const uint32_t* const sbase = x.scales + i0 / kGroupCols * x.scale_ld;
+  const uint16_t* const ybase = static_cast<const uint16_t*>(dy.ptr) + o0 + ycol;
+
+  struct Set {
+    u32x4_t x[XC], y[YC];
+    uint32_t s;
+  };
+  // As in k_weight_grad: 8 tokens follow slice k, or any slice.
+  auto load_inner = [&](Set& r, int k) {
+    const int64_t t0 = int64_t(k) * KT;
+#pragma unroll
+    for (int j = 0; j < XC; ++j) r.x[j] = gload<u32x4_t, 16>(xbase + t0 * x.ld + xoff + 16 * j);
+    r.s = gload<uint32_t, 4>(sbase + t0 + xt);
+#pragma unroll
+    for (int j = 0; j < YC; ++j) r.y[j] = gload<u32x4_t, 2>(ybase + (t0 + yt + 8 * j) * dy.ld);
+  };
+  auto load_any = [&](Set& r, int k) {
+    const int64_t t0 = int64_t(k) * KT;
+    if (t0 + KT + 8 <= tokens) return load_inner(r, k);
+    const int64_t back = t0 + xt < tokens ? 0 : tokens - 1 - (t0 + xt);  // to the last token
+#pragma unroll
+    for (int j = 0; j < XC; ++j) {
+      r.x[j] = gload<u32x4_t, 16>(xbase + (t0 + back) * x.ld + xoff + 16 * j);
+      if (back) r.x[j] = u32x4_t{0, 0, 0, 0};
+    }
+    r.s = gload<uint32_t, 4>(sbase + t0 + xt + back);
+    const int64_t n = dy.cols - o0 - ycol;
+#pragma unroll
+    for (int j = 0; j < YC; ++j) {
+      const int64_t row = t0 + yt + 8 * j;
+      const uint16_t* p = ybase + (row < tokens ? row : tokens - 1) * dy.ld;
+      if (n >= 8) {
+        r.y[j] = gload<u32x4_t, 2>(p);
+      } else {
+        uint32_t h[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) h[e] = gload<uint16_t, 2>(p + (e < n ? e : 0));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) r.y[j][e] = h[2 * e] | h[2 * e + 1] << 16;
+      }
+      if (row >= tokens) r.y[j] = u32x4_t{0, 0, 0, 0};
+    }
+  };
+
+  const uint32_t mine = lds_addr(lds) + wave * SLOT;
+  auto swz64 = [](int r) { return 4 * (r >> 1 & 1); };
+  typedef __attribute__((address_space(3))) u32x4_t lds_u32x4_t;
+  auto write = [&](const Set& r) {
+    const float s = scale_of(r.s >> xshift & 255u);
+#pragma unroll
+    for (int j = 0; j < XC; ++j)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const u32x2_t p = widen4<F>(r.x[j][2 * h], s), q = widen4<F>(r.x[j][2 * h + 1], s);
+        *(lds_u32x4_t*)(uintptr_t)(mine + xt * PITCH + (((xc / 8 + 2 * j + h) ^ swz64(xt)) << 4)) =
+            u32x4_t{p[0], p[1], q[0], q[1]};
+      }
+#pragma unroll
+    for (int j = 0; j < YC; ++j) {
+      const int row = yt + 8 * j;
+      *(lds_u32x4_t*)(uintptr_t)(mine + KT * PITCH + row * PITCH + (((lane & 7) ^ swz64(row)) << 4)) = r.y[j];
+    }
+  };
+  // Lane addresses of the four fragments (X 0, 1, dY 0, 1).
+  uint32_t fa[4];
+#pragma unroll
+  for (int f = 0; f < 4; ++f) {
+    const int si = lane & 15, g = lane >> 4;
+    const int col = 32 * (f & 1) + 16 * (g & 1) + 4 * (si & 3), kr = 8 * (g >> 1) + (si >> 2);
+    fa[f] = mine + (f < 2 ? 0 : KT * PITCH) + kr * PITCH + (((col >> 3) ^ swz64(kr)) << 4) + 8 * (si & 1);
+  }
+  f32x16_t acc[2][2];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) acc[q / 2][q % 2] = f32x16_t{};
+  u32x2_t half[2][4][2];
+  auto multiply = [&]() {
+    asm volatile("" ::: "memory");  // the slice is written first; the hardware keeps the order
+    each<16>([&](auto o) {
+      constexpr int step = o / 8, f = o / 2 % 4, r = o % 2;
+      half[step][f][r] = lds_read8_tr<(16 * step + 4 * r) * PITCH>(fa[f]);
+    });
+    each<2>([&](auto step) {
+      if constexpr (step == 0)
+        asm volatile("s_waitcnt lgkmcnt(8)" ::: "memory");  // the reads of step 1 are on their way
+      else
+        lgkm_wait();
+      u32x4_t fr[4];
+#pragma unroll
+      for (int f = 0; f < 4; ++f) {
+        hold(half[step][f][0]);
+        hold(half[step][f][1]);
+        fr[f] = __builtin_shufflevector(half[step][f][0], half[step][f][1], 0, 1, 2, 3);
+      }
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        acc[q / 2][q % 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, fr[2 + q % 2]),
+                                                                    __builtin_bit_cast(bf16x8_t, fr[q / 2]),
+                                                                    acc[q / 2][q % 2], 0, 0, 0);
+    });
+  };
+  if (count > 0) {
+    Set in[2];
+    load_any(in[0], first);
+    if (count > 1) {
+      load_inner(in[1], first - W);
+      int n = 0;
+      // Two slices ahead (past the end: the last again, unused).
+      for (; n + 1 < count; n += 2) {
+        write(in[0]);
+        load_inner(in[0], first - W * min(n + 2, count - 1));
+        multiply();
+        write(in[1]);
+        load_inner(in[1], first - W * min(n + 3, count - 1));
+        multiply();
+      }
+      if (n < count) {
+        write(in[0]);
+        multiply();
+      }
+    } else {
+      write(in[0]);
+      multiply();
+    }
+  }
+  // Quarter q goes to wave q; the sum is in the order of the waves.
+  __syncthreads();
+  f32x16_t own = {};
+  typedef __attribute__((address_space(3))) f32x4_t lds_f32x4_t;
+  auto at = [&](int q, int from) {  // the three other waves of quarter q
+    return lds_addr(lds) + ((q * 3 + (from < q ? from : from - 1)) * 4 * 64 + lane) * 16;
+  };
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const f32x16_t& a = acc[q / 2][q % 2];
+    if (wave == q) {
+      own = a;
+    } else {
+#pragma unroll
+      for (int v = 0; v < 4; ++v)
+        *(lds_f32x4_t*)(uintptr_t)(at(q, wave) + v * 1024) = f32x4_t{a[4 * v], a[4 * v + 1], a[4 * v + 2], a[4 * v + 3]};
+    }
+  }
+  __syncthreads();
+  f32x16_t total[1][1] = {};
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    if (w == wave) {
+      total[0][0] += own;
+    } else {
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        const f32x4_t p = *(const lds_f32x4_t*)(uintptr_t)(at(wave, w) + v * 1024);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) total[0][0][4 * v + e] += p[e];
+      }
+    }
+  }
+  if (t.parts > 1 && !join_parts<1, 1, W>(total, split, t.split, t.part, t.parts, wave, lane, &last)) return;
+  __syncthreads();
+  store_tile<T, 1, 1>(total, reinterpret_cast<float*>(lds) + wave * 32 * 36, dw, i0 + 32 * (wave >> 1),
+                      o0 + 32 * (wave & 1), accumulate);
+}
+
 // A tile shape's cost in us, measured on 256 CUs: starting and storing a tile,
 // and one slice of its long axis where a CU has one tile, or `full` of them or
 // more (slower where the matrix cores then clock down, faster where tiles hide
@@ -910,7 +1112,9 @@ hipError_t launch_product(DType out_t, Fp8 a_fmt, const BlocksRef& a, const Bloc
 }
 
 // Slices of 32 tokens.
-constexpr TileCost kWeightGradTiles[] = {{256, 256, 8.0, 0.64, 0.82, 1}, {128, 128, 4.0, 0.36, 0.29, 2}};
+constexpr TileCost kWeightGradTiles[] = {{256, 256, 8.0, 0.64, 0.82, 1},
+                                         {128, 128, 4.0, 0.36, 0.29, 2},
+                                         {64, 64, 3.0, 0.09, 0.09, 2}};
 
 hipError_t launch_weight_grad(DType out_t, Fp8 x_fmt, const BlocksRef& x, const DenseRef& dy, const DenseRef& dw,
                               bool accumulate, const SplitSpace& split, int cus, hipStream_t s) {
@@ -919,10 +1123,13 @@ hipError_t launch_weight_grad(DType out_t, Fp8 x_fmt, const BlocksRef& x, const 
   with_fp8(x_fmt, [&](auto fmt) {
     constexpr Fp8 F = decltype(fmt)::value;
     auto go = [&](auto k, int threads) { k<<<p.groups, threads, 0, s>>>(x, dy, dw, accumulate, p.shares, split); };
-    if (out_t == DType::BF16)
-      p.tile == 0 ? go(k_weight_grad<bf16, F, 4, 2, 2, 4>, 512) : go(k_weight_grad<bf16, F, 2, 2, 2, 2>, 256);
-    else
-      p.tile == 0 ? go(k_weight_grad<float, F, 4, 2, 2, 4>, 512) : go(k_weight_grad<float, F, 2, 2, 2, 2>, 256);
+    auto pick = [&](auto t) {
+      using T = decltype(t);
+      if (p.tile == 0) return go(k_weight_grad<T, F, 4, 2, 2, 4>, 512);
+      if (p.tile == 1) return go(k_weight_grad<T, F, 2, 2, 2, 2>, 256);
+      return go(k_weight_grad_waves<T, F>, 256);
+    };
+    out_t == DType::BF16 ? pick(bf16{}) : pick(float{});
   });
   return hipGetLastError();
 }
