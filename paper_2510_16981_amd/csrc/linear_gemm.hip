@@ -229,6 +229,15 @@ __device__ __forceinline__ bool join_parts(f32x16_t (&acc)[TM][TN], const SplitS
 // which is exact, and multiplied by 16-bit instructions at half the rate,
 // because the 8-bit instruction's sum of 64 products keeps 16 bits (measured:
 // 1.5e-5 off at K from 64 to 16384, against 5e-8 of an fp32 product).
+//
+// Tiles (chosen by `choose`): 256 x 256 on 8 waves, two a SIMD, which take
+// priority in turn (2-6% faster than equal priorities); 128 x 256 on 8 waves where
+// that fills the chip and 256 x 256 does not; 128 x 128 and 64 x 128 on 4 waves,
+// several workgroups a CU.  Large products are bound by the matrix cores (busy 64%
+// of the clocks) at the clock that their power leaves (1.69 GHz), and by the
+// tiles' stores, 6 us of 60: 8192 x 4096 x 14336 424 us, 2.27 PFLOP/s; 8192^3 2.45;
+// 4096 x 8192 x 2048 64 us.  The 4-wave tiles are bound by LDS: a slice of 128 x 128
+// is 48 KB through it, 384 clocks for 256 of MFMA.
 __device__ __forceinline__ int swz(int row) { return ((row >> 1) & 3) ^ ((row >> 3) & 1); }
 
 template <typename T, Fp8 F, int TM, int TN, int WM, int WN>
@@ -558,7 +567,13 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_product_few(BlocksRef a, Blo
 // Loads are of any alignment.  Only the last tokens, where a row's last 16 bytes
 // may end past the matrix, are read an element at a time; a part begins with its
 // last two slices, so that the loop's loads are the same for every slice (with a
-// choice between them the compiler waits for all loads in flight at each).
+// choice between them the compiler waits for all loads in flight at each: 940
+// against 1130 TFLOP/s at 8192 tokens, 14336 x 4096).
+//
+// 256 x 256 tiles on 8 waves, 128 x 128 on 4 for matrices of fewer tiles.  Bound by
+// the matrix cores (busy 65% of the clocks) at the clock that their power leaves
+// (1.59 GHz): 8192 tokens, 14336 x 4096 777 us, 1.24 PFLOP/s; 8192^3 1.31.  Unaligned
+// rows (8191) cost nothing.
 __device__ __forceinline__ int row_swz(int r) { return 4 * (r & 3); }
 
 // Each group of 16 lanes reads a 4 x 16 block of 16-bit elements; lane i gives
