@@ -185,7 +185,9 @@ muonbp_status muonbp_linear_create(const muonbp_linear_options* opt, void* hip_s
     if (c->split.sums) (void)hipFree(c->split.sums);
     if (c->split.counts) (void)hipFree(c->split.counts);
     delete c;
-    return e == hipErrorOutOfMemory ? MUONBP_E_NOMEM : MUONBP_E_HIP;
+    if (e != hipErrorOutOfMemory) return MUONBP_E_HIP;
+    (void)hipGetLastError();  // or the next launch would report it
+    return MUONBP_E_NOMEM;
   };
   hipError_t e;
   if ((e = hipGetDevice(&c->device)) != hipSuccess) return bail(e);

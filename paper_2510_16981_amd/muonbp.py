@@ -490,26 +490,27 @@ class Blocks:
     (cols rounded up to 128 at least), ``scales`` int32, ceil(cols / 512) x
     rows, a byte for each block.  Holds its tensors; makes no copy."""
 
-    __slots__ = ("_data", "_scales", "_memory", "rows", "cols", "ld", "format", "device", "ref")
+    __slots__ = ("_data", "_scales", "_memory", "rows", "cols", "ld", "format", "index", "ref")
 
     def __init__(self, data, scales, cols: int, format: int = E4M3):
         if _torch is None:
             load_library()
         rows, width = data.shape
         groups = -(-cols // GROUP_COLS)
-        if not (data.dtype is _torch.uint8 and data.is_cuda and data.stride(1) == 1
-                and width >= -(-cols // BLOCK_COLS) * BLOCK_COLS):
+        ld, inner = data.stride()
+        index = data.get_device()  # of a CPU tensor: -1
+        if (data.dtype is not _torch.uint8 or index < 0 or inner != 1
+                or width < -(-cols // BLOCK_COLS) * BLOCK_COLS):
             raise ValueError(f"data: need a CUDA uint8 matrix with rows of at least {cols} bytes rounded up "
                              f"to {BLOCK_COLS}, got {data.dtype} {tuple(data.shape)}")
-        device = data.device
-        if not (scales.shape == (groups, rows) and scales.dtype is _torch.int32
-                and scales.device == device and (rows <= 1 or scales.stride(1) == 1)):
-            raise ValueError(f"scales: need an int32 matrix of shape {(groups, rows)} on {device}, "
+        if (scales.shape != (groups, rows) or scales.dtype is not _torch.int32 or scales.get_device() != index
+                or (rows > 1 and scales.stride(1) != 1)):
+            raise ValueError(f"scales: need an int32 matrix of shape {(groups, rows)} on {data.device}, "
                              f"got {scales.dtype} {tuple(scales.shape)}")
         self._data, self._scales, self._memory = data, scales, None
-        self.rows, self.cols, self.format, self.device = rows, cols, format, device
-        self.ld = data.stride(0) if rows > 1 else width
-        self.ref = _BLOCKS.pack(data.data_ptr(), scales.data_ptr(), rows, cols, self.ld,
+        self.rows, self.cols, self.format, self.index = rows, cols, format, index
+        self.ld = ld = ld if rows > 1 else width
+        self.ref = _BLOCKS.pack(data.data_ptr(), scales.data_ptr(), rows, cols, ld,
                                 scales.stride(0) if groups > 1 else rows, format)
 
     @classmethod
@@ -518,7 +519,7 @@ class Blocks:
         self = object.__new__(cls)
         self._data = self._scales = None
         self._memory = memory
-        self.rows, self.cols, self.ld, self.format, self.device = rows, cols, ld, format, memory.device
+        self.rows, self.cols, self.ld, self.format, self.index = rows, cols, ld, format, memory.get_device()
         at = memory.data_ptr()
         self.ref = _BLOCKS.pack(at, at + rows * ld, rows, cols, ld, rows, format)
         return self
@@ -566,8 +567,9 @@ class Linear:
         if st:
             raise MuonBPError(st, "muonbp_linear_create")
         self.ctx = ctx
-        self._stream = stream
+        self._stream, self._handle = stream, stream.cuda_stream
         self.device = stream.device
+        self._index = stream.device.index
         self._codes = {torch.float32: F32, torch.bfloat16: BF16}
         # The handle of the current stream: torch.cuda.current_stream builds an
         # object for it, which takes longer than the rest of a call.
@@ -582,7 +584,7 @@ class Linear:
 
     def _dense(self, t, name: str) -> bytes:
         code = self._codes.get(t.dtype)
-        if code is None or t.dim() != 2 or t.device != self.device:
+        if code is None or t.dim() != 2 or t.get_device() != self._index:
             raise ValueError(f"{name}: need a bf16 or fp32 matrix on {self.device}, got {t.dtype} "
                              f"{tuple(t.shape)} on {t.device}")
         rows, cols = t.shape
@@ -600,13 +602,13 @@ class Linear:
         return t, _DENSE.pack(t.data_ptr(), rows, cols, cols, code)
 
     def _blocks(self, b: Blocks, name: str) -> bytes:
-        if not isinstance(b, Blocks) or b.device != self.device:
+        if not isinstance(b, Blocks) or b.index != self._index:
             raise ValueError(f"{name}: need Blocks on {self.device}")
         return b.ref
 
     def _empty(self, shape, dtype):
         torch = _torch
-        if self._current(self.device.index) == self._stream.cuda_stream:
+        if self._current(self._index) == self._handle:
             return torch.empty(shape, dtype=dtype, device=self.device)
         with torch.cuda.stream(self._stream):
             return torch.empty(shape, dtype=dtype, device=self.device)
@@ -707,7 +709,7 @@ class Linear:
     def set_stream(self, stream) -> None:
         self._check(self.lib.muonbp_linear_set_stream(self.ctx, ctypes.c_void_p(stream.cuda_stream)),
                     "set_stream")
-        self._stream = stream
+        self._stream, self._handle = stream, stream.cuda_stream
 
     def synchronize(self) -> None:
         self._check(self.lib.muonbp_linear_synchronize(self.ctx), "synchronize")

@@ -451,6 +451,17 @@ def test_without_a_workspace():
     small.close()
 
 
+def test_a_workspace_that_does_not_fit(lin):
+    """E_NOMEM, and the failed allocation's error is not left for later calls."""
+    import torch
+    from paper_2510_16981_amd import muonbp as mb
+    with pytest.raises(mb.MuonBPError) as e:
+        mb.Linear(workspace_bytes=1 << 45)
+    assert e.value.status == 4
+    x = torch.randn(3, 200, device="cuda")
+    _same_blocks(lin.quantize(x), x.double().cpu().numpy(), 0)
+
+
 def test_streams_and_graph(lin):
     """A chain on a stream of its own, then captured; every replay, with eager
     work between, gives the eager result on the inputs of the moment."""
