@@ -43,7 +43,7 @@ hipError_t launch_gated_backward(DType t, const DenseRef& dh, const BlocksRef& g
                                  const BlocksRef& dgate8, const BlocksRef& dup8, Fp8 d_fmt, hipStream_t s);
 
 // Sums of tiles whose long axis is split over workgroups: sums holds
-// sum_floats fp32 values, counts kCounts zeroed counters (left zeroed).
+// sum_floats fp32 values, counts kSplitCounts zeroed counters (left zeroed).
 struct SplitSpace {
   float* sums;
   int64_t sum_floats;
