@@ -51,9 +51,9 @@ struct SplitSpace {
 };
 constexpr int kSplitCounts = 4096;
 
-// c <- [c +] a b^T, a in fmt, b in e4m3.
+// c <- [c +] a b^T, a in fmt, b in e4m3; fp32_sums: of bf16 results too.
 hipError_t launch_product(DType out_t, Fp8 a_fmt, const BlocksRef& a, const BlocksRef& b, const DenseRef& c,
-                          bool accumulate, const SplitSpace& split, int cus, hipStream_t s);
+                          bool accumulate, bool fp32_sums, const SplitSpace& split, int cus, hipStream_t s);
 // dw <- [dw +] x^T dy, x in fmt, dy bf16.
 hipError_t launch_weight_grad(DType out_t, Fp8 x_fmt, const BlocksRef& x, const DenseRef& dy, const DenseRef& dw,
                               bool accumulate, const SplitSpace& split, int cus, hipStream_t s);

@@ -18,6 +18,7 @@ struct muonbp_linear_ctx {
   int cus = 256;
   hipStream_t stream = nullptr;
   SplitSpace split{};
+  bool fp32_sums = false;
   bool poisoned = false;
   char err[256] = "";
 };
@@ -177,10 +178,11 @@ muonbp_status muonbp_linear_create(const muonbp_linear_options* opt, void* hip_s
   muonbp_linear_options o;
   muonbp_linear_options_default(&o);
   if (opt) o = *opt;
-  if (o.workspace_bytes < 0) return MUONBP_E_INVALID;
+  if (o.workspace_bytes < 0 || (o.fp32_sums != 0 && o.fp32_sums != 1)) return MUONBP_E_INVALID;
   muonbp_linear_ctx* c = new (std::nothrow) muonbp_linear_ctx();
   if (!c) return MUONBP_E_NOMEM;
   c->stream = static_cast<hipStream_t>(hip_stream);
+  c->fp32_sums = o.fp32_sums == 1;
   auto bail = [&](hipError_t e) {
     if (c->split.sums) (void)hipFree(c->split.sums);
     if (c->split.counts) (void)hipFree(c->split.counts);
@@ -285,7 +287,8 @@ muonbp_status muonbp_linear_product(muonbp_linear_ctx* c, const muonbp_blocks* a
   sp.dense(o, size_of(t), true);
   if (sp.clash()) return fail(c, MUONBP_E_INVALID, "c overlaps an operand");
   if (o.rows == 0) return MUONBP_OK;
-  return launched(c, launch_product(t, fa, ar, br, o, accumulate == 1, c->split, c->cus, c->stream), "product");
+  return launched(
+      c, launch_product(t, fa, ar, br, o, accumulate == 1, c->fp32_sums, c->split, c->cus, c->stream), "product");
 }
 
 muonbp_status muonbp_linear_weight_grad(muonbp_linear_ctx* c, const muonbp_blocks* x, const muonbp_dense* dy,

@@ -82,7 +82,7 @@ class BlocksRef(ctypes.Structure):
 
 
 class LinearOptions(ctypes.Structure):
-    _fields_ = [("workspace_bytes", ctypes.c_int64)]
+    _fields_ = [("workspace_bytes", ctypes.c_int64), ("fp32_sums", ctypes.c_int32)]
 
 
 class Profile(ctypes.Structure):
@@ -550,9 +550,10 @@ class Linear:
 
     Matrices are 2-D CUDA tensors with contiguous rows (any row stride of at
     least cols), bf16 or fp32, or ``Blocks``.  Results not given by ``out`` are
-    allocated on the context's stream, on which every call is enqueued."""
+    allocated on the context's stream, on which every call is enqueued.
+    ``fp32_sums``: products with bf16 results add in fp32 too, at half the rate."""
 
-    def __init__(self, workspace_bytes: Optional[int] = None, stream=None):
+    def __init__(self, workspace_bytes: Optional[int] = None, stream=None, fp32_sums: bool = False):
         import torch
         self.lib = load_library()
         if stream is None:
@@ -561,6 +562,7 @@ class Linear:
         self.lib.muonbp_linear_options_default(ctypes.byref(opts))
         if workspace_bytes is not None:
             opts.workspace_bytes = int(workspace_bytes)
+        opts.fp32_sums = int(fp32_sums)
         ctx = ctypes.c_void_p()
         st = self.lib.muonbp_linear_create(ctypes.byref(opts), ctypes.c_void_p(stream.cuda_stream),
                                            ctypes.byref(ctx))
