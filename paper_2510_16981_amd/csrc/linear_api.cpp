@@ -187,9 +187,8 @@ muonbp_status muonbp_linear_create(const muonbp_linear_options* opt, void* hip_s
     if (c->split.sums) (void)hipFree(c->split.sums);
     if (c->split.counts) (void)hipFree(c->split.counts);
     delete c;
-    if (e != hipErrorOutOfMemory) return MUONBP_E_HIP;
-    (void)hipGetLastError();  // or the next launch would report it
-    return MUONBP_E_NOMEM;
+    (void)hipGetLastError();  // or the next launch of another context would report it
+    return e == hipErrorOutOfMemory ? MUONBP_E_NOMEM : MUONBP_E_HIP;
   };
   hipError_t e;
   if ((e = hipGetDevice(&c->device)) != hipSuccess) return bail(e);

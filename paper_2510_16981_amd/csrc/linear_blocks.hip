@@ -240,78 +240,67 @@ __global__ __launch_bounds__(kThreads) void k_gated_backward(DenseRef dh, Blocks
 
 // f(T{}, integral_constant<Fp8>) for the element type and format at hand.
 template <typename F>
-void with_type(DType t, F&& f) {
-  if (t == DType::F32)
-    f(float{});
-  else
-    f(bf16{});
+hipError_t with_type(DType t, F&& f) {
+  return t == DType::F32 ? f(float{}) : f(bf16{});
 }
 template <typename F>
-void with_format(Fp8 v, F&& f) {
-  if (v == Fp8::E4M3)
-    f(std::integral_constant<Fp8, Fp8::E4M3>{});
-  else
-    f(std::integral_constant<Fp8, Fp8::E5M2>{});
+hipError_t with_format(Fp8 v, F&& f) {
+  return v == Fp8::E4M3 ? f(std::integral_constant<Fp8, Fp8::E4M3>{}) : f(std::integral_constant<Fp8, Fp8::E5M2>{});
 }
 
 }  // namespace
 
 hipError_t launch_quantize(DType in_t, Fp8 fmt, const DenseRef& x, const BlocksRef& out, hipStream_t s) {
-  with_type(in_t, [&](auto t) {
-    with_format(fmt, [&](auto f) {
-      k_quantize<decltype(t), decltype(f)::value><<<strip_blocks(x.rows, x.cols), kThreads, 0, s>>>(x, out);
+  return with_type(in_t, [&](auto t) {
+    return with_format(fmt, [&](auto f) {
+      return launch(k_quantize<decltype(t), decltype(f)::value>, strip_blocks(x.rows, x.cols), kThreads, s, x, out);
     });
   });
-  return hipGetLastError();
 }
 
 hipError_t launch_quantize_weight(DType in_t, Fp8 fmt, const DenseRef& w, const BlocksRef& out,
                                   const BlocksRef& out_t, hipStream_t s) {
   const int64_t tiles =
       ((w.rows + kBlockCols - 1) / kBlockCols) * ((w.cols + kBlockCols - 1) / kBlockCols);
-  with_type(in_t, [&](auto t) {
-    with_format(fmt, [&](auto f) {
-      k_quantize_weight<decltype(t), decltype(f)::value><<<unsigned(tiles), kThreads, 0, s>>>(w, out, out_t);
+  return with_type(in_t, [&](auto t) {
+    return with_format(fmt, [&](auto f) {
+      return launch(k_quantize_weight<decltype(t), decltype(f)::value>, unsigned(tiles), kThreads, s, w, out, out_t);
     });
   });
-  return hipGetLastError();
 }
 
 hipError_t launch_restore(DType out_t, Fp8 fmt, const BlocksRef& x, const DenseRef& out, hipStream_t s) {
-  with_type(out_t, [&](auto t) {
-    with_format(fmt, [&](auto f) {
-      k_restore<decltype(t), decltype(f)::value><<<strip_blocks(x.rows, x.cols), kThreads, 0, s>>>(x, out);
+  return with_type(out_t, [&](auto t) {
+    return with_format(fmt, [&](auto f) {
+      return launch(k_restore<decltype(t), decltype(f)::value>, strip_blocks(x.rows, x.cols), kThreads, s, x, out);
     });
   });
-  return hipGetLastError();
 }
 
 hipError_t launch_gated_forward(DType t, const DenseRef& gate, const DenseRef& up, const DenseRef& h,
                                 const BlocksRef& h8, Fp8 h_fmt, const BlocksRef& gate8, const BlocksRef& up8,
                                 Fp8 kept_fmt, hipStream_t s) {
-  with_type(t, [&](auto e) {
-    with_format(kept_fmt, [&](auto fk) {
-      with_format(h_fmt, [&](auto fh) {
-        k_gated_forward<decltype(e), decltype(fk)::value, decltype(fh)::value>
-            <<<strip_blocks(gate.rows, gate.cols), kThreads, 0, s>>>(gate, up, h, h8, gate8, up8);
+  return with_type(t, [&](auto e) {
+    return with_format(kept_fmt, [&](auto fk) {
+      return with_format(h_fmt, [&](auto fh) {
+        return launch(k_gated_forward<decltype(e), decltype(fk)::value, decltype(fh)::value>,
+                      strip_blocks(gate.rows, gate.cols), kThreads, s, gate, up, h, h8, gate8, up8);
       });
     });
   });
-  return hipGetLastError();
 }
 
 hipError_t launch_gated_backward(DType t, const DenseRef& dh, const BlocksRef& gate, const BlocksRef& up,
                                  Fp8 kept_fmt, const DenseRef& dgate, const DenseRef& dup,
                                  const BlocksRef& dgate8, const BlocksRef& dup8, Fp8 d_fmt, hipStream_t s) {
-  with_type(t, [&](auto e) {
-    with_format(kept_fmt, [&](auto fk) {
-      with_format(d_fmt, [&](auto fd) {
-        k_gated_backward<decltype(e), decltype(fk)::value, decltype(fd)::value>
-            <<<strip_blocks(dh.rows, dh.cols), kThreads, 0, s>>>(dh, gate, up, dgate, dup, dgate8, dup8);
+  return with_type(t, [&](auto e) {
+    return with_format(kept_fmt, [&](auto fk) {
+      return with_format(d_fmt, [&](auto fd) {
+        return launch(k_gated_backward<decltype(e), decltype(fk)::value, decltype(fd)::value>,
+                      strip_blocks(dh.rows, dh.cols), kThreads, s, dh, gate, up, dgate, dup, dgate8, dup8);
       });
     });
   });
-  return hipGetLastError();
 }
 
 }  // namespace muonbp

@@ -2,9 +2,27 @@
 #pragma once
 #include <hip/hip_runtime.h>
 
+#include <tuple>
+
 #include "linear.h"
 
 namespace muonbp {
+
+// Launches a kernel and returns the status of that launch, which
+// hipGetLastError() after a <<<>>> is not: it also reports what an earlier call
+// of the thread left behind.  A refused launch leaves nothing behind.
+template <typename... P, typename... A>
+hipError_t launch(void (*kernel)(P...), unsigned groups, unsigned threads, hipStream_t s, const A&... args) {
+  std::tuple<P...> values(args...);
+  const hipError_t e = std::apply(
+      [&](auto&... v) {
+        void* at[] = {&v...};
+        return hipLaunchKernel(reinterpret_cast<const void*>(kernel), dim3(groups), dim3(threads), at, 0, s);
+      },
+      values);
+  if (e != hipSuccess) (void)hipGetLastError();
+  return e;
+}
 
 typedef __bf16 bf16;
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));

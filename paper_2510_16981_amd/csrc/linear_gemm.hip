@@ -1079,11 +1079,8 @@ Choice choose(const TileCost (&tiles)[N], int64_t rows, int64_t cols, int64_t sl
 }
 
 template <typename F>
-void with_fp8(Fp8 v, F&& f) {
-  if (v == Fp8::E4M3)
-    f(std::integral_constant<Fp8, Fp8::E4M3>{});
-  else
-    f(std::integral_constant<Fp8, Fp8::E5M2>{});
+hipError_t with_fp8(Fp8 v, F&& f) {
+  return v == Fp8::E4M3 ? f(std::integral_constant<Fp8, Fp8::E4M3>{}) : f(std::integral_constant<Fp8, Fp8::E5M2>{});
 }
 
 }  // namespace
@@ -1098,11 +1095,11 @@ constexpr TileCost kProductExactTiles[] = {{128, 128, 3.0, 0.37, 0.43, 2}, {64, 
 
 hipError_t launch_product(DType out_t, Fp8 a_fmt, const BlocksRef& a, const BlocksRef& b, const DenseRef& c,
                           bool accumulate, bool fp32_sums, const SplitSpace& split, int cus, hipStream_t s) {
-  with_fp8(a_fmt, [&](auto fmt) {
+  return with_fp8(a_fmt, [&](auto fmt) {
     constexpr Fp8 F = decltype(fmt)::value;
     const int64_t blocks = (a.cols + kBlockCols - 1) / kBlockCols;
     auto go = [&](auto k, const Choice& p, int threads) {
-      k<<<p.groups, threads, 0, s>>>(a, b, c, accumulate, p.shares, split);
+      return launch(k, p.groups, threads, s, a, b, c, accumulate, p.shares, split);
     };
     auto run = [&](auto t, auto exact) {
       using T = decltype(t);
@@ -1110,27 +1107,22 @@ hipError_t launch_product(DType out_t, Fp8 a_fmt, const BlocksRef& a, const Bloc
       if (c.rows <= kFewRows) {
         const unsigned groups = unsigned((a.cols + kGroupCols - 1) / kGroupCols);
         const unsigned waves = groups < unsigned(kFewWaves) ? groups : unsigned(kFewWaves);
-        k_product_few<T, F, EXACT><<<unsigned((c.cols + 15) / 16), 64 * waves, 0, s>>>(a, b, c, accumulate);
+        return launch(k_product_few<T, F, EXACT>, unsigned((c.cols + 15) / 16), 64 * waves, s, a, b, c, accumulate);
       } else if constexpr (EXACT) {
         const Choice p = choose(kProductExactTiles, c.rows, c.cols, 2 * blocks, blocks, split, cus);
         if (p.tile == 0) return go(k_product<T, F, true, 2, 2, 2, 2>, p, 256);
-        go(k_product<T, F, true, 1, 2, 2, 2>, p, 256);
+        return go(k_product<T, F, true, 1, 2, 2, 2>, p, 256);
       } else {
         const Choice p = choose(kProductTiles, c.rows, c.cols, 2 * blocks, blocks, split, cus);
         if (p.tile == 0) return go(k_product<T, F, false, 4, 2, 2, 4>, p, 512);
         if (p.tile == 1) return go(k_product<T, F, false, 2, 2, 2, 2>, p, 256);
         if (p.tile == 2) return go(k_product<T, F, false, 1, 2, 2, 2>, p, 256);
-        go(k_product<T, F, false, 2, 2, 2, 4>, p, 512);
+        return go(k_product<T, F, false, 2, 2, 2, 4>, p, 512);
       }
     };
-    if (out_t == DType::F32)
-      run(float{}, std::true_type{});
-    else if (fp32_sums)
-      run(bf16{}, std::true_type{});
-    else
-      run(bf16{}, std::false_type{});
+    if (out_t == DType::F32) return run(float{}, std::true_type{});
+    return fp32_sums ? run(bf16{}, std::true_type{}) : run(bf16{}, std::false_type{});
   });
-  return hipGetLastError();
 }
 
 // Slices of 32 tokens.
@@ -1142,18 +1134,19 @@ hipError_t launch_weight_grad(DType out_t, Fp8 x_fmt, const BlocksRef& x, const 
                               bool accumulate, const SplitSpace& split, int cus, hipStream_t s) {
   const int64_t slices = (x.rows + 31) / 32;
   const Choice p = choose(kWeightGradTiles, dw.rows, dw.cols, slices, slices > 0 ? slices : 1, split, cus);
-  with_fp8(x_fmt, [&](auto fmt) {
+  return with_fp8(x_fmt, [&](auto fmt) {
     constexpr Fp8 F = decltype(fmt)::value;
-    auto go = [&](auto k, int threads) { k<<<p.groups, threads, 0, s>>>(x, dy, dw, accumulate, p.shares, split); };
+    auto go = [&](auto k, int threads) {
+      return launch(k, p.groups, threads, s, x, dy, dw, accumulate, p.shares, split);
+    };
     auto pick = [&](auto t) {
       using T = decltype(t);
       if (p.tile == 0) return go(k_weight_grad<T, F, 4, 2, 2, 4>, 512);
       if (p.tile == 1) return go(k_weight_grad<T, F, 2, 2, 2, 2>, 256);
       return go(k_weight_grad_waves<T, F>, 256);
     };
-    out_t == DType::BF16 ? pick(bf16{}) : pick(float{});
+    return out_t == DType::BF16 ? pick(bf16{}) : pick(float{});
   });
-  return hipGetLastError();
 }
 
 }  // namespace muonbp
