@@ -461,7 +461,8 @@ void muonbp_adamw_destroy(muonbp_adamw_ctx* ctx); /* NULL is a no-op */
  * may be captured into a HIP graph.  Calls of one context share its workspace
  * and run on its stream in order.  Outputs must not overlap inputs or each
  * other (E_INVALID).  rows = 0 is valid everywhere (weight_grad over no tokens
- * gives zeros); its pointers may then be NULL.
+ * gives zeros); its pointers may then be NULL.  The largest matrix, dense or
+ * 8-bit, has rows ceil(cols / 512) <= 2^26 - 4 and cols <= 2^22 (E_SHAPE).
  * ---------------------------------------------------------------------- */
 typedef enum { MUONBP_E4M3 = 0, MUONBP_E5M2 = 1 } muonbp_format;
 

@@ -25,10 +25,12 @@ struct muonbp_linear_ctx {
 
 namespace {
 
-// Limits of the kernels' index arithmetic: 32-bit offsets inside a tile of 256
-// rows, and a launch of fewer than 2^32 threads.
+// Limits of the kernels' index arithmetic, 32-bit offsets inside a tile of 256
+// rows, and of a launch, fewer than 2^32 threads: a wave for each row and 512
+// columns, in workgroups of four.
 constexpr int64_t kMaxCols = int64_t(1) << 22;
-constexpr int64_t kMaxRows = int64_t(1) << 26;
+constexpr int64_t kMaxStrips = (int64_t(1) << 26) - 4;
+static_assert((kMaxStrips + 3) / 4 * 256 < int64_t(1) << 32, "launch");
 
 __attribute__((format(printf, 3, 4))) muonbp_status fail(muonbp_linear_ctx* c, muonbp_status st, const char* fmt,
                                                          ...) {
@@ -112,9 +114,9 @@ muonbp_status check_dense(muonbp_linear_ctx* c, const muonbp_dense* m, const cha
   if (m->dtype != MUONBP_BF16 && (bf16_only || m->dtype != MUONBP_F32))
     return fail(c, MUONBP_E_DTYPE, "%s: unsupported dtype", name);
   const int64_t es = m->dtype == MUONBP_F32 ? 4 : 2;
-  if (m->rows < 0 || m->rows > kMaxRows || m->cols < 1 || m->cols > kMaxCols)
-    return fail(c, MUONBP_E_SHAPE, "%s: rows 0..2^26 and cols 1..2^22", name);
-  if (m->ld < m->cols || m->ld > (int64_t(1) << 32) || m->rows * groups_of(m->cols) > kMaxRows)
+  if (m->rows < 0 || m->rows > kMaxStrips || m->cols < 1 || m->cols > kMaxCols)
+    return fail(c, MUONBP_E_SHAPE, "%s: rows 0..2^26 - 4 and cols 1..2^22", name);
+  if (m->ld < m->cols || m->ld > (int64_t(1) << 32) || m->rows * groups_of(m->cols) > kMaxStrips)
     return fail(c, MUONBP_E_SHAPE, "%s: ld below cols or over 2^32, or a matrix too large", name);
   if (m->rows > 0 && !m->ptr) return fail(c, MUONBP_E_INVALID, "%s: NULL pointer", name);
   if (reinterpret_cast<uintptr_t>(m->ptr) % uintptr_t(es))
@@ -128,10 +130,10 @@ muonbp_status check_blocks(muonbp_linear_ctx* c, const muonbp_blocks* m, const c
   if (!m) return fail(c, MUONBP_E_INVALID, "%s must not be NULL", name);
   if (m->format != MUONBP_E4M3 && m->format != MUONBP_E5M2)
     return fail(c, MUONBP_E_INVALID, "%s: unknown format", name);
-  if (m->rows < 0 || m->rows > kMaxRows || m->cols < 1 || m->cols > kMaxCols)
-    return fail(c, MUONBP_E_SHAPE, "%s: rows 0..2^26 and cols 1..2^22", name);
+  if (m->rows < 0 || m->rows > kMaxStrips || m->cols < 1 || m->cols > kMaxCols)
+    return fail(c, MUONBP_E_SHAPE, "%s: rows 0..2^26 - 4 and cols 1..2^22", name);
   if (m->ld < padded(m->cols) || m->ld % 16 || m->ld > kMaxCols || m->scale_ld < m->rows ||
-      m->scale_ld > (int64_t(1) << 31) || m->rows * groups_of(m->cols) > kMaxRows)
+      m->scale_ld > (int64_t(1) << 31) || m->rows * groups_of(m->cols) > kMaxStrips)
     return fail(c, MUONBP_E_SHAPE, "%s: ld below the padded cols, no multiple of 16 or too large, or scale_ld below rows",
                 name);
   if (m->rows > 0 && (!m->data || !m->scales)) return fail(c, MUONBP_E_INVALID, "%s: NULL pointer", name);
