@@ -550,7 +550,11 @@ class Linear:
 
     Matrices are 2-D CUDA tensors with contiguous rows (any row stride of at
     least cols), bf16 or fp32, or ``Blocks``.  Results not given by ``out`` are
-    allocated on the context's stream, on which every call is enqueued.
+    allocated on the context's stream, on which every call is enqueued.  A call made
+    while another stream is current comes after that stream's work so far and
+    before its later work, so operands and results may be made, used and freed
+    there as with torch's own operators (to overlap the two streams, make the
+    context's the current one and order them yourself).
     ``fp32_sums``: products with bf16 results add in fp32 too, at half the rate."""
 
     def __init__(self, workspace_bytes: Optional[int] = None, stream=None, fp32_sums: bool = False):
@@ -584,6 +588,32 @@ class Linear:
             detail = self.lib.muonbp_linear_last_error(self.ctx)
             raise MuonBPError(st, f"{what}: {detail.decode() if detail else ''}")
 
+    def _join(self):
+        """The context's stream waits for the current one, which is another;
+        returns the current one, None where the two may not meet."""
+        cuda = _torch.cuda
+        with cuda.stream(self._stream):
+            captured = cuda.is_current_stream_capturing()
+        if captured != cuda.is_current_stream_capturing():
+            if captured:  # by a program that captures it alone: nothing runs now
+                return None
+            if self._handle == 0:
+                raise ValueError("the default stream cannot be captured: set_stream to the one that is")
+        current = cuda.current_stream(self._index)
+        self._stream.wait_stream(current)
+        return current
+
+    def _run(self, call, what: str, *args):
+        if self._current(self._index) == self._handle:
+            st = call(self.ctx, *args)
+        else:
+            current = self._join()
+            st = call(self.ctx, *args)
+            if current is not None:
+                current.wait_stream(self._stream)
+        if st:
+            self._check(st, what)
+
     def _dense(self, t, name: str) -> bytes:
         code = self._codes.get(t.dtype)
         if code is None or t.dim() != 2 or t.get_device() != self._index:
@@ -612,6 +642,7 @@ class Linear:
         torch = _torch
         if self._current(self._index) == self._handle:
             return torch.empty(shape, dtype=dtype, device=self.device)
+        self._join()  # first: under capture the memory is the graph's
         with torch.cuda.stream(self._stream):
             return torch.empty(shape, dtype=dtype, device=self.device)
 
@@ -627,7 +658,7 @@ class Linear:
         d = self._dense(x, "x")
         if out is None:
             out = self.empty_blocks(x.shape[0], x.shape[1], format)
-        self._check(self.lib.muonbp_linear_quantize(self.ctx, d, self._blocks(out, "out")), "quantize")
+        self._run(self.lib.muonbp_linear_quantize, "quantize", d, self._blocks(out, "out"))
         return out
 
     def quantize_weight(self, w, format: int = E4M3, out: Optional[Blocks] = None,
@@ -639,8 +670,8 @@ class Linear:
             out = self.empty_blocks(rows, cols, format)
         if out_t is None:
             out_t = self.empty_blocks(cols, rows, format)
-        self._check(self.lib.muonbp_linear_quantize_weight(self.ctx, d, self._blocks(out, "out"),
-                                                           self._blocks(out_t, "out_t")), "quantize_weight")
+        self._run(self.lib.muonbp_linear_quantize_weight, "quantize_weight", d, self._blocks(out, "out"),
+                  self._blocks(out_t, "out_t"))
         return out, out_t
 
     def restore(self, x: Blocks, dtype=None, out=None):
@@ -650,7 +681,7 @@ class Linear:
             out, d = self._new(x.rows, x.cols, dtype or _torch.bfloat16)
         else:
             d = self._dense(out, "out")
-        self._check(self.lib.muonbp_linear_restore(self.ctx, px, d), "restore")
+        self._run(self.lib.muonbp_linear_restore, "restore", px, d)
         return out
 
     def _product(self, call, what, pa, pb, rows, cols, dtype, out, accumulate):
@@ -660,7 +691,7 @@ class Linear:
             out, d = self._new(rows, cols, dtype or _torch.bfloat16)
         else:
             d = self._dense(out, "out")
-        self._check(call(self.ctx, pa, pb, d, accumulate), what)
+        self._run(call, what, pa, pb, d, accumulate)
         return out
 
     def product(self, a: Blocks, b: Blocks, dtype=None, out=None, accumulate: bool = False):
@@ -690,7 +721,7 @@ class Linear:
         if keep:
             kept = self.empty_blocks(rows, cols, format), self.empty_blocks(rows, cols, format)
             g8, u8 = kept[0].ref, kept[1].ref
-        self._check(self.lib.muonbp_linear_gated_forward(self.ctx, g, u, d, h8, g8, u8), "gated_forward")
+        self._run(self.lib.muonbp_linear_gated_forward, "gated_forward", g, u, d, h8, g8, u8)
         return h, kept[0], kept[1]
 
     def gated_backward(self, dh, gate: Blocks, up: Blocks, blocks: bool = False, format: int = E4M3):
@@ -700,12 +731,10 @@ class Linear:
         rows, cols = dh.shape
         (dgate, a), (dup, b) = self._new(rows, cols, dh.dtype), self._new(rows, cols, dh.dtype)
         if not blocks:
-            self._check(self.lib.muonbp_linear_gated_backward(self.ctx, d, pg, pu, a, b, None, None),
-                        "gated_backward")
+            self._run(self.lib.muonbp_linear_gated_backward, "gated_backward", d, pg, pu, a, b, None, None)
             return dgate, dup
         dgate8, dup8 = self.empty_blocks(rows, cols, format), self.empty_blocks(rows, cols, format)
-        self._check(self.lib.muonbp_linear_gated_backward(self.ctx, d, pg, pu, a, b, dgate8.ref, dup8.ref),
-                    "gated_backward")
+        self._run(self.lib.muonbp_linear_gated_backward, "gated_backward", d, pg, pu, a, b, dgate8.ref, dup8.ref)
         return dgate, dup, dgate8, dup8
 
     def set_stream(self, stream) -> None:
