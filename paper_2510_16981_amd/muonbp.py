@@ -496,11 +496,10 @@ class Blocks:
         if _torch is None:
             load_library()
         rows, width = data.shape
-        groups = -(-cols // GROUP_COLS)
+        groups, padded = -(-cols // GROUP_COLS), -(-cols // BLOCK_COLS) * BLOCK_COLS
         ld, inner = data.stride()
         index = data.get_device()  # of a CPU tensor: -1
-        if (data.dtype is not _torch.uint8 or index < 0 or inner != 1
-                or width < -(-cols // BLOCK_COLS) * BLOCK_COLS):
+        if data.dtype is not _torch.uint8 or index < 0 or inner != 1 or width < padded:
             raise ValueError(f"data: need a CUDA uint8 matrix with rows of at least {cols} bytes rounded up "
                              f"to {BLOCK_COLS}, got {data.dtype} {tuple(data.shape)}")
         if (scales.shape != (groups, rows) or scales.dtype is not _torch.int32 or scales.get_device() != index
@@ -509,7 +508,7 @@ class Blocks:
                              f"got {scales.dtype} {tuple(scales.shape)}")
         self._data, self._scales, self._memory = data, scales, None
         self.rows, self.cols, self.format, self.index = rows, cols, format, index
-        self.ld = ld = ld if rows > 1 else width
+        self.ld = ld = ld if rows > 1 else padded  # of one row: its width may be no multiple of 16
         self.ref = _BLOCKS.pack(data.data_ptr(), scales.data_ptr(), rows, cols, ld,
                                 scales.stride(0) if groups > 1 else rows, format)
 
