@@ -632,6 +632,11 @@ class Linear:
             raise ValueError(f"need bf16 or fp32, got {dtype}")
         return t, _DENSE.pack(t.data_ptr(), rows, cols, cols, code)
 
+    def _given(self, out, dtype) -> bytes:
+        if dtype is not None and out.dtype != dtype:
+            raise ValueError(f"out is {out.dtype}, not {dtype}")
+        return self._dense(out, "out")
+
     def _blocks(self, b: Blocks, name: str) -> bytes:
         if not isinstance(b, Blocks) or b.index != self._index:
             raise ValueError(f"{name}: need Blocks on {self.device}")
@@ -652,19 +657,28 @@ class Linear:
                           format)
 
     # -- API
-    def quantize(self, x, format: int = E4M3, out: Optional[Blocks] = None) -> Blocks:
-        """x in 8 bits, one scale for each block of 128 columns of a row."""
+    def quantize(self, x, format: Optional[int] = None, out: Optional[Blocks] = None) -> Blocks:
+        """x in 8 bits (E4M3, or out's format), one scale for each block of 128
+        columns of a row."""
         d = self._dense(x, "x")
         if out is None:
-            out = self.empty_blocks(x.shape[0], x.shape[1], format)
+            out = self.empty_blocks(x.shape[0], x.shape[1], E4M3 if format is None else format)
+        elif format is not None and out.format != format:
+            raise ValueError(f"out is in format {out.format}, not {format}")
         self._run(self.lib.muonbp_linear_quantize, "quantize", d, self._blocks(out, "out"))
         return out
 
-    def quantize_weight(self, w, format: int = E4M3, out: Optional[Blocks] = None,
+    def quantize_weight(self, w, format: Optional[int] = None, out: Optional[Blocks] = None,
                         out_t: Optional[Blocks] = None) -> Tuple[Blocks, Blocks]:
-        """(w, its transpose) in 8 bits, one scale for each 128 x 128 tile."""
+        """(w, its transpose) in 8 bits (E4M3, or the format of what is given),
+        one scale for each 128 x 128 tile."""
         d = self._dense(w, "w")
         rows, cols = w.shape
+        given = [b.format for b in (out, out_t) if b is not None]
+        if format is None:
+            format = given[0] if given else E4M3
+        if any(f != format for f in given):
+            raise ValueError(f"out and out_t are in formats {given}, not {format}")
         if out is None:
             out = self.empty_blocks(rows, cols, format)
         if out_t is None:
@@ -674,12 +688,12 @@ class Linear:
         return out, out_t
 
     def restore(self, x: Blocks, dtype=None, out=None):
-        """The values of x (bf16 by default), exact."""
+        """The values of x (bf16, or out's type), exact."""
         px = self._blocks(x, "x")
         if out is None:
             out, d = self._new(x.rows, x.cols, dtype or _torch.bfloat16)
         else:
-            d = self._dense(out, "out")
+            d = self._given(out, dtype)
         self._run(self.lib.muonbp_linear_restore, "restore", px, d)
         return out
 
@@ -689,18 +703,18 @@ class Linear:
                 raise ValueError("accumulate needs out")
             out, d = self._new(rows, cols, dtype or _torch.bfloat16)
         else:
-            d = self._dense(out, "out")
+            d = self._given(out, dtype)
         self._run(call, what, pa, pb, d, accumulate)
         return out
 
     def product(self, a: Blocks, b: Blocks, dtype=None, out=None, accumulate: bool = False):
-        """a b^T (bf16 by default); ``accumulate`` adds it to ``out``."""
+        """a b^T (bf16, or out's type); ``accumulate`` adds it to ``out``."""
         pa, pb = self._blocks(a, "a"), self._blocks(b, "b")
         return self._product(self.lib.muonbp_linear_product, "product", pa, pb, a.rows, b.rows, dtype, out,
                              accumulate)
 
     def weight_grad(self, x: Blocks, dy, dtype=None, out=None, accumulate: bool = False):
-        """x^T dy (bf16 by default); ``accumulate`` adds it to ``out``."""
+        """x^T dy (bf16, or out's type); ``accumulate`` adds it to ``out``."""
         px, pd = self._blocks(x, "x"), self._dense(dy, "dy")
         return self._product(self.lib.muonbp_linear_weight_grad, "weight_grad", px, pd, x.cols, dy.shape[1], dtype,
                              out, accumulate)
