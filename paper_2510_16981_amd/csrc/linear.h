@@ -6,12 +6,9 @@
 #include <cstdint>
 
 #include "kernels.h"
+#include "linear_plan.h"
 
 namespace muonbp {
-
-// Columns that share a scale, and those whose scales share a 32-bit word.
-constexpr int kBlockCols = 128;
-constexpr int kGroupCols = 4 * kBlockCols;
 
 enum class Fp8 { E4M3 = 0, E5M2 = 1 };
 
@@ -49,7 +46,6 @@ struct SplitSpace {
   int64_t sum_floats;
   int* counts;
 };
-constexpr int kSplitCounts = 4096;
 
 // c <- [c +] a b^T, a in fmt, b in e4m3; fp32_sums: of bf16 results too.
 hipError_t launch_product(DType out_t, Fp8 a_fmt, const BlocksRef& a, const BlocksRef& b, const DenseRef& c,

@@ -69,13 +69,6 @@ __device__ __forceinline__ uint32_t lds_addr(const void* p) {
   return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((const lds_void_t*)p));
 }
 
-// How a grid of tall x wide tiles is shared out: the first `whole` tiles to one
-// workgroup each, the others, their long axis in `parts`, to `parts` workgroups
-// each.
-struct Shares {
-  int whole, parts;
-};
-
 // Which tile and part workgroup b runs.  Consecutive workgroups go to the 8 XCDs
 // in turn; each XCD gets a contiguous run of tiles, taken `kGroupTall` tiles
 // high, so that the tiles resident on one XCD share rows and columns in its L2.
@@ -170,7 +163,6 @@ __device__ __forceinline__ void store_tile(f32x16_t (&acc)[TM][TN], float* st, c
 // (they bypass the per-XCD caches), and every store has completed before the
 // part is counted.  False: this workgroup is done.
 constexpr int kCoherent = 16;  // sc1
-constexpr int kMaxParts = 8;
 template <int TM, int TN, int W>
 __device__ __forceinline__ bool join_parts(f32x16_t (&acc)[TM][TN], const SplitSpace& split, int tile, int part,
                                            int parts, int wave, int lane, int* last) {
@@ -235,7 +227,7 @@ __device__ __forceinline__ bool join_parts(f32x16_t (&acc)[TM][TN], const SplitS
 // of the largest of their eight; in the 2-norm, at any K, 1.1e-5 to 1.6e-5 for normal
 // values and 4e-5 to 1e-4 with outlier channels, where rounding to bf16 costs 1.7e-3.
 //
-// Tiles (chosen by `choose`): 256 x 256 on 8 waves, two a SIMD, which take
+// Tiles (chosen in linear_plan.h): 256 x 256 on 8 waves, two a SIMD, which take
 // priority in turn (2-6% faster than equal priorities); 128 x 256 on 8 waves where
 // that fills the chip and 256 x 256 does not; 128 x 128 and 64 x 128 on 4 waves,
 // several workgroups a CU.  Large products are bound by the matrix cores (busy 64%
@@ -460,7 +452,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_product(BlocksRef a, BlocksRef
 // meet in LDS.  Measured, one row: 14336 x 4096 14.5 us (4.0 TB/s), 4096 x 14336
 // 11.2 us (5.2 TB/s); 2 and 8 waves took 14.7 and 16.8, 12.5 and 11.1 us, and
 // columns split over 2 or 4 workgroups 13.9 and 23 us, 13.1 and 14.1 us.
-constexpr int kFewRows = 16, kFewWaves = 4;
+constexpr int kFewWaves = 4;
 
 template <typename T, Fp8 F, bool EXACT>
 __global__ __launch_bounds__(64 * kFewWaves) void k_product_few(BlocksRef a, BlocksRef b, DenseRef c,
@@ -1023,61 +1015,6 @@ __global__ __launch_bounds__(256) void k_weight_grad_waves(BlocksRef x, DenseRef
                       o0 + 32 * (wave & 1), accumulate);
 }
 
-// A tile shape's cost in us, measured on 256 CUs: starting and storing a tile,
-// and one slice of its long axis where a CU has one tile, or `full` of them or
-// more (slower where the matrix cores then clock down, faster where tiles hide
-// each other's waits).  Joining parts writes and reads all their sums, at 5 TB/s.
-struct TileCost {
-  int bm, bn;
-  double start, slice, slice_full;
-  int full;
-  // Of `groups` workgroups that run `slices` each, all on the chip together or
-  // in rounds.
-  double rounds(int64_t groups, double slices, int cus) const {
-    const double load = double(groups) / cus - (full - 1);
-    const double at = load < 0.0 ? 0.0 : load > 1.0 ? 1.0 : load;
-    return double((groups + cus - 1) / cus) * (start + (slice + (slice_full - slice) * at) * slices);
-  }
-  double us(const Shares& s, int64_t tiles, int64_t slices, int cus) const {
-    const int64_t groups = (tiles - s.whole) * s.parts;
-    double t = rounds(groups, double((slices + s.parts - 1) / s.parts), cus);
-    if (s.whole) t += rounds(s.whole, double(slices), cus);
-    return s.parts > 1 ? t + 1.0 + 0.4 * s.parts + 8.0 * double(groups) * bm * bn / 5e6 : t;
-  }
-};
-
-struct Choice {
-  int tile;
-  Shares shares;
-  unsigned groups;
-};
-
-// The tile shape and the shares that cost least: no tile, every tile, or the
-// tiles of the last, unfilled round in parts.
-template <int N>
-Choice choose(const TileCost (&tiles)[N], int64_t rows, int64_t cols, int64_t slices, int64_t most_parts,
-              const SplitSpace& split, int cus) {
-  Choice best{};
-  double least = -1.0;
-  for (int t = 0; t < N; ++t) {
-    const int64_t bm = tiles[t].bm, bn = tiles[t].bn;
-    const int64_t count = (rows + bm - 1) / bm * ((cols + bn - 1) / bn);
-    for (int parts = 1; parts <= kMaxParts && parts <= most_parts; ++parts)
-      for (int tail = 0; tail < 2; ++tail) {
-        const int64_t whole = tail ? count / cus * cus : 0, cut = count - whole;
-        if (tail && (parts == 1 || whole == 0 || cut == 0)) continue;
-        if (parts > 1 && (cut > kSplitCounts || cut * parts * bm * bn > split.sum_floats)) continue;
-        const Shares s{int(whole), parts};
-        const double us = tiles[t].us(s, count, slices, cus);
-        if (least < 0.0 || us < least) {
-          least = us;
-          best = Choice{t, s, unsigned(whole + cut * parts)};
-        }
-      }
-  }
-  return best;
-}
-
 template <typename F>
 hipError_t with_fp8(Fp8 v, F&& f) {
   return v == Fp8::E4M3 ? f(std::integral_constant<Fp8, Fp8::E4M3>{}) : f(std::integral_constant<Fp8, Fp8::E5M2>{});
@@ -1085,19 +1022,10 @@ hipError_t with_fp8(Fp8 v, F&& f) {
 
 }  // namespace
 
-// Slices of 64 columns, in 8 bits; widened (EXACT): half the rate, so the 256 x 256
-// tile, whose widened fragments do not fit its registers, is left out.
-constexpr TileCost kProductTiles[] = {{256, 256, 8.0, 0.50, 0.78, 1},
-                                      {128, 128, 2.5, 0.25, 0.28, 2},
-                                      {64, 128, 1.0, 0.18, 0.20, 2},
-                                      {128, 256, 5.0, 0.32, 0.46, 1}};
-constexpr TileCost kProductExactTiles[] = {{128, 128, 3.0, 0.37, 0.43, 2}, {64, 128, 1.0, 0.27, 0.29, 2}};
-
 hipError_t launch_product(DType out_t, Fp8 a_fmt, const BlocksRef& a, const BlocksRef& b, const DenseRef& c,
                           bool accumulate, bool fp32_sums, const SplitSpace& split, int cus, hipStream_t s) {
   return with_fp8(a_fmt, [&](auto fmt) {
     constexpr Fp8 F = decltype(fmt)::value;
-    const int64_t blocks = (a.cols + kBlockCols - 1) / kBlockCols;
     auto go = [&](auto k, const Choice& p, int threads) {
       return launch(k, p.groups, threads, s, a, b, c, accumulate, p.shares, split);
     };
@@ -1108,12 +1036,12 @@ hipError_t launch_product(DType out_t, Fp8 a_fmt, const BlocksRef& a, const Bloc
         const unsigned groups = unsigned((a.cols + kGroupCols - 1) / kGroupCols);
         const unsigned waves = groups < unsigned(kFewWaves) ? groups : unsigned(kFewWaves);
         return launch(k_product_few<T, F, EXACT>, unsigned((c.cols + 15) / 16), 64 * waves, s, a, b, c, accumulate);
-      } else if constexpr (EXACT) {
-        const Choice p = choose(kProductExactTiles, c.rows, c.cols, 2 * blocks, blocks, split, cus);
+      }
+      const Choice p = product_choice(EXACT, c.rows, c.cols, a.cols, split.sum_floats, cus);
+      if constexpr (EXACT) {
         if (p.tile == 0) return go(k_product<T, F, true, 2, 2, 2, 2>, p, 256);
         return go(k_product<T, F, true, 1, 2, 2, 2>, p, 256);
       } else {
-        const Choice p = choose(kProductTiles, c.rows, c.cols, 2 * blocks, blocks, split, cus);
         if (p.tile == 0) return go(k_product<T, F, false, 4, 2, 2, 4>, p, 512);
         if (p.tile == 1) return go(k_product<T, F, false, 2, 2, 2, 2>, p, 256);
         if (p.tile == 2) return go(k_product<T, F, false, 1, 2, 2, 2>, p, 256);
@@ -1125,15 +1053,9 @@ hipError_t launch_product(DType out_t, Fp8 a_fmt, const BlocksRef& a, const Bloc
   });
 }
 
-// Slices of 32 tokens.
-constexpr TileCost kWeightGradTiles[] = {{256, 256, 8.0, 0.64, 0.82, 1},
-                                         {128, 128, 4.0, 0.36, 0.29, 2},
-                                         {64, 64, 3.0, 0.09, 0.09, 2}};
-
 hipError_t launch_weight_grad(DType out_t, Fp8 x_fmt, const BlocksRef& x, const DenseRef& dy, const DenseRef& dw,
                               bool accumulate, const SplitSpace& split, int cus, hipStream_t s) {
-  const int64_t slices = (x.rows + 31) / 32;
-  const Choice p = choose(kWeightGradTiles, dw.rows, dw.cols, slices, slices > 0 ? slices : 1, split, cus);
+  const Choice p = weight_grad_choice(dw.rows, dw.cols, x.rows, split.sum_floats, cus);
   return with_fp8(x_fmt, [&](auto fmt) {
     constexpr Fp8 F = decltype(fmt)::value;
     auto go = [&](auto k, int threads) {
