@@ -457,12 +457,15 @@ void muonbp_adamw_destroy(muonbp_adamw_ctx* ctx); /* NULL is a no-op */
  * precision.  A block of zeros has e = -110.
  *
  * The conventions above apply (status codes, asynchrony on the context's
- * stream, no synchronisation, thread safety).  A call allocates nothing, so it
- * may be captured into a HIP graph.  Calls of one context share its workspace
- * and run on its stream in order.  Outputs must not overlap inputs or each
- * other (E_INVALID).  rows = 0 is valid everywhere (weight_grad over no tokens
- * gives zeros); its pointers may then be NULL.  The largest matrix, dense or
- * 8-bit, has rows ceil(cols / 512) <= 2^26 - 4 and cols <= 2^22 (E_SHAPE).
+ * stream, no synchronisation, thread safety).  Calls of one context share its
+ * workspace and run on its stream in order.  A call allocates nothing, so it may be
+ * captured into a HIP graph; the graph uses the context's workspace, so order its
+ * replays with all other work of the context (replay on its stream, or wait), also
+ * with each other, and replay none after muonbp_linear_destroy.  Outputs must not
+ * overlap inputs or each other (E_INVALID).  Activations of no rows are valid
+ * (weight_grad over no tokens gives zeros), and their pointers may then be NULL; a
+ * weight of no rows, or a product's b, is not (E_SHAPE).  The largest matrix, dense
+ * or 8-bit, has rows ceil(cols / 512) <= 2^26 - 4 and cols <= 2^22 (E_SHAPE).
  * ---------------------------------------------------------------------- */
 typedef enum { MUONBP_E4M3 = 0, MUONBP_E5M2 = 1 } muonbp_format;
 
@@ -515,7 +518,8 @@ muonbp_status muonbp_linear_quantize(muonbp_linear_ctx* ctx, const muonbp_dense*
                                      const muonbp_blocks* out);
 
 /* out <- w in 8 bits with one scale for each 128 x 128 tile, and out_t <- its
- * transpose (the same values; cols x rows).  Either may be NULL, not both. */
+ * transpose (the same values; cols x rows).  Either may be NULL, not both.  (Of
+ * e5m2 weights muonbp_linear_product takes no b.) */
 muonbp_status muonbp_linear_quantize_weight(muonbp_linear_ctx* ctx, const muonbp_dense* w,
                                             const muonbp_blocks* out, const muonbp_blocks* out_t);
 
@@ -540,10 +544,9 @@ muonbp_status muonbp_linear_product(muonbp_linear_ctx* ctx, const muonbp_blocks*
                                     int32_t accumulate);
 
 /* dw <- x^T dy (accumulate = 0) or dw + x^T dy (1): x is tokens x I in 8 bits
- * (the kept activations), dy tokens x O in bf16 (ld at most 2^25), dw I x O in
- * bf16 or f32.  The
- * values of x are exact in bf16, so the only roundings are those of the fp32
- * sum and of dw. */
+ * (the kept activations), dy tokens x O in bf16 (ld at most 2^25; gated_backward
+ * gives such gradients of a dh in bf16), dw I x O in bf16 or f32.  The values of x
+ * are exact in bf16, so the only roundings are those of the fp32 sum and of dw. */
 muonbp_status muonbp_linear_weight_grad(muonbp_linear_ctx* ctx, const muonbp_blocks* x,
                                         const muonbp_dense* dy, const muonbp_dense* dw,
                                         int32_t accumulate);

@@ -1,14 +1,14 @@
 // Kernels between 16- or 32-bit matrices and 8-bit blocks, and the gated
 // activation with 8-bit checkpoints.  All stream their operands once and are
-// bound by memory: 16384 x 4096 quantized in 38 us (5.4 TB/s) and restored in 31
-// (6.5), gated 8192 x 14336 forward in 165 us (5.7) and backward in 168 (5.6); a
-// large copy reaches 4.97.
+// bound by memory (traced, inputs not cached): 16384 x 4096 quantized in 39 us
+// (5.2 TB/s) and restored in 30 (6.6), gated 8192 x 14336 forward in 165 us (5.7) and
+// backward in 169 (5.6); a large copy reaches 4.97.
 //
 // One wave holds one row of one group of 512 columns: lane l has columns 8 l ..
 // 8 l + 7 (16 bytes of bf16 in, 8 bytes out), 16 lanes one block of 128, and the
-// wave one word of scales.  (Two or four rows a wave were no faster on any size:
-// 16384 x 4096 quantized in 35.4 against 34.7 us, 64 x 4096 in 3.6 against 2.5;
-// gated forward 107 against 102 and 4.7 against 3.5.)
+// wave one word of scales.  (Two or four rows a wave were no faster: in a loop over
+// the same buffers, partly cached, 16384 x 4096 quantized in 35.4 against 34.7 us,
+// 64 x 4096 in 3.6 against 2.5.)
 #include "linear_device.h"
 
 namespace muonbp {
@@ -106,8 +106,8 @@ __global__ __launch_bounds__(kThreads) void k_restore(BlocksRef x, DenseRef out)
 
 // One workgroup a 128 x 128 tile: thread t has columns 8 (t % 16) .. + 7 of rows
 // t / 16, 16 + t / 16, ...; the tile's max through LDS, then the values in rows
-// and, through LDS, in columns.  4096 x 14336 in bf16 to both layouts: 51 us
-// (4.6 TB/s).
+// and, through LDS, in columns.  4096 x 14336 in bf16 to both layouts: 52 us
+// (4.5 TB/s).
 constexpr int kTilePitch = kBlockCols + 4;
 
 template <typename T, Fp8 F>

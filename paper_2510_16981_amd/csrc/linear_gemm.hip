@@ -158,10 +158,19 @@ __device__ __forceinline__ void store_tile(f32x16_t (&acc)[TM][TN], float* st, c
 
 // The parts of a tile whose long axis is split: every workgroup stores its
 // sums, the last to arrive adds them in the order of the parts (the result does
-// not depend on which is last) and goes on; the others end.  Sums are stored and
-// loaded 16 bytes a lane with the device-coherent policy of a relaxed atomic
-// (they bypass the per-XCD caches), and every store has completed before the
-// part is counted.  False: this workgroup is done.
+// not depend on which is last) and goes on; the others end, and none waits for
+// another (false: this workgroup is done).  Sums are stored and loaded 16 bytes a
+// lane with the policy of a relaxed atomic of device scope (sc1).  Why the last one reads what was stored:
+//  - A store of that scope is complete (vmcnt 0) once it is at the device's point
+//    of coherence, past the XCD's L2; each wave waits for its own, then the
+//    workgroup for its waves, and only then is the part counted.
+//  - The counts are read-modify-writes of device scope, one after another: who
+//    gets parts - 1 comes after every other part's count, and its loads are
+//    issued after that (the barrier).
+//  - A load of that scope takes no line of the CU's cache, and none of its XCD's
+//    L2 could be stale: a line of sums is touched by one part's stores and then by
+//    these loads, once in a launch (parts are multiples of 16 KB, so no line
+//    is shared), and what earlier launches left was invalidated at this one's start.
 constexpr int kCoherent = 16;  // sc1
 template <int TM, int TN, int W>
 __device__ __forceinline__ bool join_parts(f32x16_t (&acc)[TM][TN], const SplitSpace& split, int tile, int part,
@@ -231,10 +240,11 @@ __device__ __forceinline__ bool join_parts(f32x16_t (&acc)[TM][TN], const SplitS
 // priority in turn (2-6% faster than equal priorities); 128 x 256 on 8 waves where
 // that fills the chip and 256 x 256 does not; 128 x 128 and 64 x 128 on 4 waves,
 // several workgroups a CU.  Large products are bound by the matrix cores (busy 64%
-// of the clocks) at the clock that their power leaves (1.69 GHz), and by the
-// tiles' stores, 6 us of 60: 8192 x 4096 x 14336 424 us, 2.27 PFLOP/s; 8192^3 2.45;
-// 4096 x 8192 x 2048 64 us.  The 4-wave tiles are bound by LDS: a slice of 128 x 128
-// is 48 KB through it, 384 clocks for 256 of MFMA.
+// of the clocks) at the clock that their power leaves (1.69 GHz), which differs by the
+// card, and by the tiles' stores, 6 us of 60: 8192 x 4096 x 14336 414 to 443 us on four
+// cards (2.17 to 2.32 PFLOP/s), 4096 x 8192 x 2048 62 to 67; EXACT 789 and 123.  The
+// 4-wave tiles are bound by LDS: a slice of 128 x 128 is 48 KB through it, 384 clocks
+// for 256 of MFMA.
 __device__ __forceinline__ int swz(int row) { return ((row >> 1) & 3) ^ ((row >> 3) & 1); }
 
 template <typename T, Fp8 F, bool EXACT, int TM, int TN, int WM, int WN>
@@ -449,9 +459,11 @@ __global__ __launch_bounds__(64 * WM * WN) void k_product(BlocksRef a, BlocksRef
 // One workgroup holds 16 rows of B; its waves take the groups of 512 columns in
 // turn, straight from memory into registers (16 bytes a lane, 64 contiguous
 // bytes of a row an instruction) with the next group on its way, and their sums
-// meet in LDS.  Measured, one row: 14336 x 4096 14.5 us (4.0 TB/s), 4096 x 14336
-// 11.2 us (5.2 TB/s); 2 and 8 waves took 14.7 and 16.8, 12.5 and 11.1 us, and
-// columns split over 2 or 4 workgroups 13.9 and 23 us, 13.1 and 14.1 us.
+// meet in LDS.  Measured in a loop over the same operands (59 MB, which the last
+// cache holds), one row: 14336 x 4096 12.5 us, 4096 x 14336 11.4 us; EXACT 13.0 and 11.8.
+// 2 and 8 waves took 14.7 and 16.8 where 4 took 14.5, 12.5 and 11.1 where 4 took 11.2,
+// and columns split over 2 or 4 workgroups 13.9 and 23 us, 13.1 and 14.1 us.  Few
+// columns of C leave CUs without work: 1024 x 4096 4.5 us, 1024 x 14336 9.9.
 constexpr int kFewWaves = 4;
 
 template <typename T, Fp8 F, bool EXACT>
@@ -567,8 +579,8 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_product_few(BlocksRef a, Blo
 //
 // 256 x 256 tiles on 8 waves, 128 x 128 on 4 for matrices of fewer tiles.  Bound by
 // the matrix cores (busy 65% of the clocks) at the clock that their power leaves
-// (1.59 GHz): 8192 tokens, 14336 x 4096 777 us, 1.24 PFLOP/s; 8192^3 1.31.  Unaligned
-// rows (8191) cost nothing.
+// (1.59 GHz), which differs by the card: 8192 tokens, 14336 x 4096 755 to 817 us on four
+// cards (1.18 to 1.27 PFLOP/s); 8192^3 839 to 889.  Unaligned rows (8191) cost nothing.
 __device__ __forceinline__ int row_swz(int r) { return 4 * (r & 3); }
 
 // Each group of 16 lanes reads a 4 x 16 block of 16-bit elements; lane i gives
