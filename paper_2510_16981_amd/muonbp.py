@@ -548,13 +548,12 @@ class Linear:
     """The 8-bit linear-layer operators on one stream (muonbp_linear_*).
 
     Matrices are 2-D CUDA tensors with contiguous rows (any row stride of at
-    least cols), bf16 or fp32, or ``Blocks``.  Results not given by ``out`` are
-    allocated on the context's stream, on which every call is enqueued.  A call made
-    while another stream is current comes after that stream's work so far and
-    before its later work, so operands and results may be made, used and freed
-    there as with torch's own operators (to overlap the two streams, make the
-    context's the current one and order them yourself).  A captured graph that
-    holds calls uses the context's workspace: its replays are to be ordered with
+    least cols), bf16 or fp32, or ``Blocks``.  Every call is enqueued on the
+    context's stream; results not given by ``out`` are allocated on the current
+    one.  Where that is another, the call comes after its work so far and before its
+    later work, so operands and results are made, used and freed there as with
+    torch's own operators (to overlap the two streams, make the context's the
+    current one and order them yourself).  A captured graph that holds calls uses the context's workspace: its replays are to be ordered with
     all other calls and replays of the context, and none may follow ``close``.
     Results are not part of torch's autograd, whatever the operands require.
     ``fp32_sums``: products with bf16 results add in fp32 too, at half the rate."""
@@ -646,12 +645,7 @@ class Linear:
         return b.ref
 
     def _empty(self, shape, dtype):
-        torch = _torch
-        if self._current(self._index) == self._handle:
-            return torch.empty(shape, dtype=dtype, device=self.device)
-        self._join()  # first: under capture the memory is the graph's
-        with torch.cuda.stream(self._stream):
-            return torch.empty(shape, dtype=dtype, device=self.device)
+        return _torch.empty(shape, dtype=dtype, device=self.device)
 
     def empty_blocks(self, rows: int, cols: int, format: int = E4M3) -> Blocks:
         """Uninitialised Blocks of rows x cols."""

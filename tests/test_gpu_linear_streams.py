@@ -61,6 +61,26 @@ def test_memory_freed_on_the_current_stream(own):
         assert float(low) == float(high) == k + 1
 
 
+def test_a_result_belongs_to_the_current_stream(own):
+    """Dropped while the current stream has yet to read it, its memory is not
+    taken by what the context's stream makes next."""
+    import torch
+    n = 2048
+    kept = own.quantize(torch.full((n, n), 3.0, device="cuda"))
+    torch.cuda.synchronize()
+    for _ in range(3):
+        y = own.restore(kept, dtype=torch.float32)
+        _busy()
+        low = y.amin()
+        del y
+        with torch.cuda.stream(own._stream):
+            taken = [torch.full((n, n), -1.0, device="cuda") for _ in range(3)]
+            taken.append(own.restore(kept, dtype=torch.float32))
+        assert float(low) == 3.0
+        torch.cuda.synchronize()
+        del taken
+
+
 def test_capture_on_the_current_stream(own):
     """A graph captured on a stream that is not the context's holds the calls;
     every replay gives the eager result on the inputs of the moment."""
