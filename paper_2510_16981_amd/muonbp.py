@@ -553,10 +553,13 @@ class Linear:
     one.  Where that is another, the call comes after its work so far and before its
     later work, so operands and results are made, used and freed there as with
     torch's own operators (to overlap the two streams, make the context's the
-    current one and order them yourself).  A captured graph that holds calls uses the context's workspace: its replays are to be ordered with
-    all other calls and replays of the context, and none may follow ``close``.
-    Results are not part of torch's autograd, whatever the operands require.
-    ``fp32_sums``: products with bf16 results add in fp32 too, at half the rate."""
+    current one and order them yourself).
+
+    A captured graph that holds calls uses the context's workspace: its replays are
+    to be ordered with all other calls and replays of the context, and none may
+    follow ``close``.  Results are not part of torch's autograd, whatever the
+    operands require.  ``fp32_sums``: products with bf16 results add in fp32 too,
+    at half the rate."""
 
     def __init__(self, workspace_bytes: Optional[int] = None, stream=None, fp32_sums: bool = False):
         import torch
